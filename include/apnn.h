@@ -262,6 +262,131 @@ int apnn_sumpool(const uint32_t *X_dev, int64_t N, int64_t H, int64_t W, int64_t
 int apnn_sumpool_fc(const uint32_t *X_dev, int64_t N, int64_t H, int64_t W, int64_t C, int bits,
                     const uint32_t *W_dev, int64_t Cout, int p, apnn_encoding encW, int32_t *Y_dev, void *stream);
 
+/* ---- 8-bit products with a scale for each token and channel ---------------- */
+
+/* Element type of dense operands and results. */
+typedef enum { APNN_F32 = 0, APNN_F16 = 1, APNN_BF16 = 2 } apnn_dtype;
+
+/* Bytes between the rows of 8-bit codes: K rounded up to 16.  Bytes K and up of
+ * a row are 0.  0 on bad input. */
+int64_t apnn_token_pitch(int64_t K);
+
+/* 8-bit codes of a rows x K matrix with one scale for each row:
+ *   a = max_k |x[r][k]|,  scale[r] = a / 127,
+ *   code[r][k] = x[r][k] * 127 / a rounded to the nearest integer, half to even
+ * (the quotient is decided exactly, so equal inputs give equal codes everywhere).
+ * A row of zeros has codes and scale 0.  A row that holds a NaN or an infinity
+ * has codes 0 and scale NaN, so that every product of it is NaN.
+ * src_dev: row r starts ld elements (>= K) after row r - 1.  codes_dev: int8
+ * [rows][apnn_token_pitch(K)], 16-byte aligned, fully written; scale_dev: fp32
+ * [rows].  Activations and, once, weights (a row is then an output channel). */
+int apnn_quantize_tokens(const void *src_dev, apnn_dtype type, int64_t rows, int64_t K, int64_t ld,
+                         int8_t *codes_dev, float *scale_dev, void *stream);
+
+/* Y[m][n] = x_scale[m] * w_scale[n] * sum_k X[m][k] W[n][k] + bias[n], the sum in
+ * int32 (exact), the rest in 64 bits, rounded to the result's type.
+ * X_dev: int8 [M][pitch], W_dev: int8 [N][pitch], pitch = apnn_token_pitch(K), both
+ * 16-byte aligned, bytes K and up of a row 0; any int8 code, -128 among them.
+ * bias_dev: fp32 [N] or NULL.  Y_dev: row m starts ldy elements (>= N) after row
+ * m - 1; elements N and up of a row are left as they were.  K = 0 gives the bias.
+ * APNN_ERR_OVERFLOW if K 2^14 >= 2^31. */
+int apnn_gemm_scaled(const int8_t *X_dev, const float *x_scale_dev, const int8_t *W_dev, const float *w_scale_dev,
+                     const float *bias_dev, void *Y_dev, apnn_dtype type, int64_t M, int64_t N, int64_t K, int64_t ldy,
+                     void *stream);
+
+/* ---- a paged key/value cache of 4-bit codes, and the attention that reads it -- */
+
+/* A key or value row of one (token, head) is D codes of 4 bits in groups of 32
+ * channels, each group with a power of two as its scale:
+ *   value = magnitude * 2^e, magnitudes 0 .5 1 1.5 2 3 4 6 by the code's low three
+ *   bits, its high bit the sign (FP4 E2M1); scale byte e + 127 (E8M0), e in -23..13.
+ * Channel c sits in byte c / 2 of the row, even channels in the low nibble.  Every
+ * value of the cache is exact in fp16 and in bf16.
+ * A token's slot is page * page_size + place in the page.  A (token, head) whose
+ * key scale bytes are 255 is held as NaN, key and value.
+ * All four arrays 16-byte aligned. */
+typedef struct {
+    uint8_t *k_codes_dev;  /* [pages][heads][page_size][D / 2]  */
+    uint8_t *k_scale_dev;  /* [pages][heads][page_size][D / 32] */
+    uint8_t *v_codes_dev;  /* as the keys'                      */
+    uint8_t *v_scale_dev;
+    int64_t pages;         /* at most 2^31 - 1                  */
+    int heads;             /* 1 .. 1024                         */
+    int page_size;         /* 16, 32, 64, 128 or 256 tokens     */
+    int D;                 /* 64, 96, 128 or 256 channels       */
+} apnn_kv_cache;
+
+/* New tokens of a layer: dense keys, values and queries.  Strides in elements;
+ * the channels of a head are adjacent. */
+typedef struct {
+    int64_t tokens;
+    apnn_dtype type;
+    const void *k_dev, *v_dev;  /* [tokens][cache heads][D] */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int64_t *slot_dev;    /* [tokens]: where each token goes */
+    /* Position rotation of the first `rot` channels (even, at most D; 0: none): pairs
+     * (i, i + rot / 2), or with `interleaved` (2 i, 2 i + 1), become
+     * (a cos - b sin, b cos + a sin), computed in 64 bits and rounded to fp32.
+     * Row p of the table: rot / 2 cosines, then rot / 2 sines, of position p. */
+    int rot, interleaved;
+    const float *table_dev;     /* [table_rows][rot] */
+    int64_t table_rows;
+    const int32_t *position_dev;/* [tokens] */
+    /* Queries rotated like the keys and written to q_out; q_heads 0: none.
+     * q_out may be q itself, with the same strides. */
+    int q_heads;
+    const void *q_dev;          /* [tokens][q_heads][D] */
+    void *q_out_dev;
+    int64_t q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+} apnn_kv_tokens;
+
+/* Rotates, quantises and writes tokens into their slots:
+ *   e = the least exponent in -23..13 with max|x| < 7 * 2^e over the group (7 is half
+ *   way from the largest magnitude, 6, to the 8 that is missing), code = the magnitude
+ *   nearest to |x| / 2^e, ties to the even code, 6 at most.
+ * A (token, head) whose rotated key or value is not finite in fp32 is held as NaN.
+ * A token whose slot lies outside the cache (a negative one marks padding), or whose
+ * position lies outside the table (looked at if rot > 0), is left out: nothing of it is
+ * written, q_out neither.  Slots of one call must differ: of two tokens in one slot,
+ * that slot holds a mixture. */
+int apnn_kv_append(const apnn_kv_cache *cache, const apnn_kv_tokens *tokens, void *stream);
+
+/* The values that slots hold: k_out_dev, v_out_dev [n][heads][D], 16-byte aligned, either may be NULL.
+ * Slots outside the cache give zeros. */
+int apnn_kv_read(const apnn_kv_cache *cache, const int64_t *slot_dev, int64_t n, void *k_out_dev, void *v_out_dev,
+                 apnn_dtype type, void *stream);
+
+typedef struct {
+    int64_t tokens;             /* rows of q and out */
+    apnn_dtype type;            /* APNN_F16 or APNN_BF16, of q and out */
+    int q_heads;                /* a multiple of the cache's heads; head h reads cache head h / (q_heads / heads) */
+    const void *q_dev;          /* [tokens][q_heads][D], strides in elements, channels adjacent */
+    void *out_dev;              /* must not overlap q */
+    int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    int64_t seqs;
+    const int32_t *q_start_dev; /* [seqs + 1]: sequence b's queries are rows q_start[b] .. q_start[b + 1] - 1; NULL: one each */
+    const int32_t *len_dev;     /* [seqs]: tokens of the sequence in the cache, its queries' own among them */
+    const int32_t *page_dev;    /* [seqs][max_pages]: token t of sequence b is in page page[b][t / page_size] */
+    int64_t max_pages;
+    int64_t max_q;              /* no sequence has more queries (1 if q_start_dev is NULL) */
+    float scale;                /* of the scores, finite */
+} apnn_kv_attention_desc;
+
+/* out = sum_t softmax_t(scale * q . k_t) v_t for every query head.  Query i of the n of a
+ * sequence of l tokens stands at position l - n + i and sees the tokens at positions 0 up
+ * to its own; one that sees none (l < n, l = 0) gets zeros.  Scores, softmax and sums are
+ * held in fp32; the softmax's weights meet the values rounded to fp16, 11 bits.
+ * Unseen tokens count for nothing whatever their keys and values hold; one that holds NaN
+ * and is seen makes the query's result NaN.
+ * Rows of out that no sequence has are left as they were, and so are queries beyond
+ * max_q.  Tokens beyond the table's max_pages, and tokens of pages outside the cache, are
+ * never read and count as unseen.
+ * workspace_dev: apnn_kv_attention_workspace_bytes(desc, cache) bytes, 16-byte aligned (0
+ * bytes: may be NULL), of this call alone until it has run. */
+size_t apnn_kv_attention_workspace_bytes(const apnn_kv_attention_desc *desc, const apnn_kv_cache *cache);
+int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_kv_cache *cache, void *workspace_dev,
+                      size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

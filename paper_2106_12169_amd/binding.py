@@ -15,7 +15,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Tuple
 
 import torch
 
@@ -32,6 +32,8 @@ EXPORTS = (
     "apnn_pack_patch_weights", "apnn_quantize", "apnn_gemm", "apnn_conv2d", "apnn_layer",
     "apnn_layer_pair", "apnn_input_weight_bytes", "apnn_pack_input_weights", "apnn_input_layer",
     "apnn_fold_bn", "apnn_maxpool", "apnn_sumpool", "apnn_sumpool_fc", "apnn_workspace_bytes",
+    "apnn_token_pitch", "apnn_quantize_tokens", "apnn_gemm_scaled", "apnn_kv_append", "apnn_kv_read", "apnn_kv_attention",
+    "apnn_kv_attention_workspace_bytes",
     "apnn_debug_force", "apnn_debug_reset", "apnn_debug_tile_choice",
 )
 
@@ -74,6 +76,26 @@ class LayerDesc(C.Structure):
                 ("acc_out_dev", C.c_void_p), ("float_out_dev", C.c_void_p), ("pool", C.c_int)]
 
 
+class KVCacheDesc(C.Structure):
+    _fields_ = [("k_codes_dev", C.c_void_p), ("k_scale_dev", C.c_void_p), ("v_codes_dev", C.c_void_p), ("v_scale_dev", C.c_void_p),
+                ("pages", C.c_int64), ("heads", C.c_int), ("page_size", C.c_int), ("D", C.c_int)]
+
+
+class KVTokensDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("type", C.c_int), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("slot_dev", C.c_void_p), ("rot", C.c_int), ("interleaved", C.c_int), ("table_dev", C.c_void_p), ("table_rows", C.c_int64),
+                ("position_dev", C.c_void_p), ("q_heads", C.c_int), ("q_dev", C.c_void_p), ("q_out_dev", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("q_out_token_stride", C.c_int64), ("q_out_head_stride", C.c_int64)]
+
+
+class KVAttentionDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("type", C.c_int), ("q_heads", C.c_int), ("q_dev", C.c_void_p), ("out_dev", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64),
+                ("seqs", C.c_int64), ("q_start_dev", C.c_void_p), ("len_dev", C.c_void_p), ("page_dev", C.c_void_p),
+                ("max_pages", C.c_int64), ("max_q", C.c_int64), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -113,13 +135,23 @@ def lib():
     L.apnn_sumpool_fc.argtypes = [vp, i64, i64, i64, i64, i32, vp, i64, i32, i32, vp, vp]
     L.apnn_workspace_bytes.restype = C.c_size_t
     L.apnn_workspace_bytes.argtypes = [C.POINTER(LayerDesc)]
+    L.apnn_token_pitch.restype = i64
+    L.apnn_token_pitch.argtypes = [i64]
+    L.apnn_quantize_tokens.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    L.apnn_gemm_scaled.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, vp]
+    L.apnn_kv_append.argtypes = [C.POINTER(KVCacheDesc), C.POINTER(KVTokensDesc), vp]
+    L.apnn_kv_read.argtypes = [C.POINTER(KVCacheDesc), vp, i64, vp, vp, i32, vp]
+    L.apnn_kv_attention_workspace_bytes.restype = C.c_size_t
+    L.apnn_kv_attention_workspace_bytes.argtypes = [C.POINTER(KVAttentionDesc), C.POINTER(KVCacheDesc)]
+    L.apnn_kv_attention.argtypes = [C.POINTER(KVAttentionDesc), C.POINTER(KVCacheDesc), vp, C.c_size_t, vp]
     L.apnn_debug_force.argtypes = [C.c_char_p, i32]
     L.apnn_debug_reset.restype = None
     L.apnn_debug_reset.argtypes = []
     L.apnn_debug_tile_choice.argtypes = [i64, i64, i32, i32]
     for name in EXPORTS:
         if name not in ("apnn_last_error", "apnn_row_words", "apnn_packed_words", "apnn_fmap_words",
-                        "apnn_input_weight_bytes", "apnn_workspace_bytes", "apnn_debug_reset"):
+                        "apnn_input_weight_bytes", "apnn_workspace_bytes", "apnn_debug_reset", "apnn_token_pitch",
+                        "apnn_kv_attention_workspace_bytes"):
             getattr(L, name).restype = i32
     _lib = L
     return L
@@ -328,6 +360,100 @@ def apnn_sumpool_fc(X: torch.Tensor, N: int, H: int, W: int, Cc: int, bits: int,
     if out is None:
         out = torch.empty((N, Cout), dtype=torch.int32, device=X.device)
     _N.sumpool_fc(X, N, H, W, Cc, bits, Wp, Cout, p, encW, out)
+    return out
+
+
+def apnn_token_pitch(K: int) -> int:
+    """Bytes of a row of 8-bit codes: K rounded up to 16."""
+    return lib().apnn_token_pitch(K)
+
+
+def apnn_quantize_tokens(src: torch.Tensor, codes: Optional[torch.Tensor] = None,
+                         scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """src: rows x K (float32, float16 or bfloat16; any row stride) -> int8 codes [rows][apnn_token_pitch(K)] and fp32 scales
+    [rows], row = codes * scale.  Activations of a call, and weights (output channels x K) once."""
+    if codes is None:
+        codes = torch.empty((src.shape[0], -(-src.shape[1] // 16) * 16), dtype=torch.int8, device=src.device)
+    if scale is None:
+        scale = torch.empty(src.shape[0], dtype=torch.float32, device=src.device)
+    _N.quantize_tokens(src, codes, scale)
+    return codes, scale
+
+
+def apnn_gemm_scaled(X: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, K: int, *,
+                     bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """X: M x K, W: N x K codes as apnn_quantize_tokens lays them out -> M x N of `dtype` (or into `out`, of any row stride)."""
+    if out is None:
+        out = torch.empty((X.shape[0], W.shape[0]), dtype=dtype, device=X.device)
+    _N.gemm_scaled(X, x_scale, W, w_scale, K, bias, out)
+    return out
+
+
+@dataclass
+class KVCache:
+    """The four arrays of a paged 4-bit key/value cache (uint8; layout in include/apnn.h)."""
+    k_codes: torch.Tensor       # [pages][heads][page_size][D / 2]
+    k_scale: torch.Tensor       # [pages][heads][page_size][D / 32]
+    v_codes: torch.Tensor
+    v_scale: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, D: int, device="cuda") -> "KVCache":
+        """A cache without tokens: every slot holds zeros."""
+        return cls(*(torch.zeros((pages, heads, page_size, n), dtype=torch.uint8, device=device) for n in (D // 2, D // 32, D // 2, D // 32)))
+
+    @property
+    def heads(self) -> int:
+        return self.k_codes.shape[1]
+
+    @property
+    def page_size(self) -> int:
+        return self.k_codes.shape[2]
+
+    @property
+    def D(self) -> int:
+        return 2 * self.k_codes.shape[3]
+
+
+def apnn_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *,
+                   positions: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None, interleaved: bool = False,
+                   q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """k, v: tokens x heads x D into the cache's slots (int64, page * page_size + place; negative: padding, left out).
+    table (fp32, positions x rot: cosines, then sines) and positions (int32) rotate the first rot channels of keys and of q
+    (tokens x query heads x D).  Returns the rotated queries (q_out, which may be q itself; made if not given), None without q."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _N.kv_append(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, k, v, slots, positions, table, interleaved, q, q_out)
+    return q_out
+
+
+def apnn_kv_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The keys and values that slots (int64) hold, each len(slots) x heads x D; zeros for slots outside the cache."""
+    k, v = (torch.empty((slots.shape[0], cache.heads, cache.D), dtype=dtype, device=slots.device) for _ in range(2))
+    _N.kv_read(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, slots, k, v)
+    return k, v
+
+
+def apnn_kv_attention_workspace_bytes(cache: KVCache, tokens: int, q_heads: int, seqs: int, max_pages: int, *,
+                                      ragged: bool = False, max_q: int = 1) -> int:
+    """Bytes apnn_kv_attention needs for calls of these sizes (ragged: with q_start)."""
+    return _N.kv_attention_workspace(cache.heads, cache.page_size, cache.D, tokens, q_heads, seqs, max_pages, ragged, max_q)
+
+
+def apnn_kv_attention(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, pages: torch.Tensor, scale: float, *,
+                      q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q: tokens x query heads x D (float16 or bfloat16) -> the same, attended.  lens: int32, tokens in the cache of each
+    sequence, its queries' own among them; pages: int32, sequences x max_pages.  q_start: int32, sequences + 1, where each
+    sequence's queries begin (None: one query each); max_q: a bound on the queries of a sequence (default: all of them,
+    which is right but spreads the work for one sequence that has them all).  Rows of `out` that no sequence has are left as
+    they were.  workspace: uint8, for the caller to keep (default: allocated for the call)."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if max_q is None:
+        max_q = q.shape[0] if q_start is not None else 1
+    _N.kv_attention(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
     return out
 
 

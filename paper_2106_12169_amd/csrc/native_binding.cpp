@@ -9,6 +9,8 @@
 //
 // As with ctypes, the interpreter lock is released while the library runs (a launch can wait for queue space).
 #include <Python.h>
+#include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -373,6 +375,309 @@ PyObject *py_sumpool_fc(PyObject *, PyObject *const *args, Py_ssize_t n)    // (
     return call([&](void *st) { return apnn_sumpool_fc(X, N, H, W, C, bits, Wt, Cout, p, static_cast<apnn_encoding>(encW), out, st); });
 }
 
+// ---- operators on typed tensors (8-bit products with scales, the 4-bit cache): their sizes, types and strides are the tensors'
+// own, so they are checked here; what the library checks itself is left to it.  All tensors of a call lie on one device, whose
+// current stream is used whichever device is current.
+
+class Tensors {
+public:
+    Tensors(PyObject *const *a, Py_ssize_t n, Py_ssize_t want) : a_(a)
+    {
+        if (n != want) fail(PyExc_TypeError, "%zd arguments expected, got %zd", want, n);
+    }
+    bool ok() const { return ok_; }
+    PyObject *object() { return a_[i_++]; }
+
+    // The next argument as a device tensor of `dim` dimensions (any number: -1) whose last one is contiguous; null for None where that may be.
+    const at::Tensor *strided(const char *name, int dim, bool optional = false)
+    {
+        if (!ok_) return nullptr;
+        PyObject *o = object();
+        if (optional && o == Py_None) return nullptr;
+        if (!THPVariable_Check(o)) return fail(PyExc_TypeError, "%s: a torch tensor is expected", name);
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!t.is_cuda()) return fail(PyExc_AssertionError, "%s: a device tensor is expected", name);
+        if (dim >= 0 && t.dim() != dim) return fail(PyExc_ValueError, "%s: %d dimensions are expected, got %lld", name, dim, static_cast<long long>(t.dim()));
+        if (t.dim() && t.size(-1) > 1 && t.stride(-1) != 1) return fail(PyExc_AssertionError, "%s: the last dimension has to be contiguous", name);
+        for (int64_t s : t.strides())
+            if (s < 0) return fail(PyExc_ValueError, "%s: negative stride", name);
+        if (!have_device_) { device_ = t.device(); have_device_ = true; }
+        if (t.device() != device_) return fail(PyExc_ValueError, "%s: on another device than the call's other tensors", name);
+        return &t;
+    }
+    // The same, contiguous as a whole and of type `type`.
+    const at::Tensor *dense(const char *name, int dim, at::ScalarType type, bool optional = false)
+    {
+        const at::Tensor *t = strided(name, dim, optional);
+        if (!t) return nullptr;
+        if (t->scalar_type() != type) return fail(PyExc_TypeError, "%s: type %s is expected, got %s", name, c10::toString(type), c10::toString(t->scalar_type()));
+        if (!t->is_contiguous()) return fail(PyExc_AssertionError, "%s: a contiguous tensor is expected", name);
+        return t;
+    }
+    // fp32, fp16 or bf16
+    apnn_dtype type(const char *name, const at::Tensor *t)
+    {
+        if (!ok_ || !t) return APNN_F32;
+        switch (t->scalar_type()) {
+            case at::kFloat: return APNN_F32;
+            case at::kHalf: return APNN_F16;
+            case at::kBFloat16: return APNN_BF16;
+            default: fail(PyExc_TypeError, "%s: float32, float16 or bfloat16 is expected, got %s", name, c10::toString(t->scalar_type())); return APNN_F32;
+        }
+    }
+    void same_type(const char *name, const at::Tensor *t, const at::Tensor *as)
+    {
+        if (ok_ && t && as && t->scalar_type() != as->scalar_type())
+            fail(PyExc_TypeError, "%s: type %s is expected, got %s", name, c10::toString(as->scalar_type()), c10::toString(t->scalar_type()));
+    }
+    void sizes(const char *name, const at::Tensor *t, at::IntArrayRef want)
+    {
+        if (!ok_ || !t) return;
+        if (t->sizes() == want) return;
+        char is[64], be[64];
+        text(is, sizeof is, t->sizes());
+        text(be, sizeof be, want);
+        fail(PyExc_ValueError, "%s: size (%s) is expected, got (%s)", name, be, is);
+    }
+    long long integer()
+    {
+        if (!ok_) return 0;
+        PyObject *n = PyNumber_Index(object());
+        const long long v = n ? PyLong_AsLongLong(n) : 0;
+        Py_XDECREF(n);
+        if (PyErr_Occurred()) ok_ = false;
+        return v;
+    }
+    float real()
+    {
+        if (!ok_) return 0.0f;
+        const double v = PyFloat_AsDouble(object());
+        if (v == -1.0 && PyErr_Occurred()) ok_ = false;
+        return static_cast<float>(v);
+    }
+    template <class... A> std::nullptr_t fail(PyObject *error, const char *format, A... a)
+    {
+        if (ok_) PyErr_Format(error, format, a...);
+        ok_ = false;
+        return nullptr;
+    }
+    at::Device device() const { return device_; }
+
+    // Calls the library on the tensors' device: f(stream).
+    template <class F> PyObject *call(F &&f)
+    {
+        const c10::DeviceGuard guard(device_);
+        void *stream = static_cast<void *>(c10::hip::getCurrentHIPStream(device_.index()).stream());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = f(stream);
+        Py_END_ALLOW_THREADS
+        return finish(rc);
+    }
+
+private:
+    static void text(char *to, size_t room, at::IntArrayRef v)
+    {
+        size_t at = 0;
+        to[0] = 0;
+        for (size_t i = 0; i < v.size() && at < room; ++i) at += static_cast<size_t>(snprintf(to + at, room - at, i ? ", %lld" : "%lld", static_cast<long long>(v[i])));
+    }
+
+    PyObject *const *a_;
+    Py_ssize_t i_ = 0;
+    bool ok_ = true, have_device_ = false;
+    at::Device device_ = at::Device(at::kCUDA, 0);
+};
+
+template <class T> T *data(const at::Tensor *t) { return t ? static_cast<T *>(t->data_ptr()) : nullptr; }
+
+PyObject *py_quantize_tokens(PyObject *, PyObject *const *args, Py_ssize_t n)   // (src, codes, scale)
+{
+    Tensors a(args, n, 3);
+    const at::Tensor *src = a.strided("src", 2), *codes = a.dense("codes", 2, at::kChar), *scale = a.dense("scale", 1, at::kFloat);
+    const apnn_dtype type = a.type("src", src);
+    if (!a.ok()) return nullptr;
+    const int64_t rows = src->size(0), K = src->size(1), ld = rows > 1 ? src->stride(0) : K;
+    a.sizes("codes", codes, {rows, apnn_token_pitch(K)});
+    a.sizes("scale", scale, {rows});
+    if (!a.ok()) return nullptr;
+    return a.call([&](void *st) { return apnn_quantize_tokens(data<void>(src), type, rows, K, ld, data<int8_t>(codes), data<float>(scale), st); });
+}
+
+PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)       // (X, x_scale, W, w_scale, K, bias, out)
+{
+    Tensors a(args, n, 7);
+    const at::Tensor *X = a.dense("X", 2, at::kChar), *xs = a.dense("x_scale", 1, at::kFloat), *W = a.dense("W", 2, at::kChar), *ws = a.dense("w_scale", 1, at::kFloat);
+    const int64_t K = a.integer();
+    const at::Tensor *bias = a.dense("bias", 1, at::kFloat, true), *out = a.strided("out", 2);
+    const apnn_dtype type = a.type("out", out);
+    if (!a.ok()) return nullptr;
+    const int64_t M = X->size(0), N = W->size(0), pitch = apnn_token_pitch(K);
+    a.sizes("X", X, {M, pitch});
+    a.sizes("W", W, {N, pitch});
+    a.sizes("x_scale", xs, {M});
+    a.sizes("w_scale", ws, {N});
+    a.sizes("bias", bias, {N});
+    a.sizes("out", out, {M, N});
+    if (!a.ok()) return nullptr;
+    const int64_t ldy = M > 1 ? out->stride(0) : N;
+    return a.call([&](void *st) {
+        return apnn_gemm_scaled(data<int8_t>(X), data<float>(xs), data<int8_t>(W), data<float>(ws), data<float>(bias), data<void>(out), type, M, N, K, ldy, st);
+    });
+}
+
+// the four arrays of a binding.KVCache
+apnn_kv_cache read_cache(Tensors &a)
+{
+    apnn_kv_cache c = {};
+    const at::Tensor *kc = a.dense("k_codes", 4, at::kByte), *ks = a.dense("k_scale", 4, at::kByte), *vc = a.dense("v_codes", 4, at::kByte), *vs = a.dense("v_scale", 4, at::kByte);
+    if (!a.ok()) return c;
+    const int64_t pages = kc->size(0), heads = kc->size(1), page = kc->size(2), D = 2 * kc->size(3);
+    a.sizes("k_scale", ks, {pages, heads, page, D / 32});
+    a.sizes("v_codes", vc, {pages, heads, page, D / 2});
+    a.sizes("v_scale", vs, {pages, heads, page, D / 32});
+    if (!a.ok()) return c;
+    c.k_codes_dev = data<uint8_t>(kc);
+    c.k_scale_dev = data<uint8_t>(ks);
+    c.v_codes_dev = data<uint8_t>(vc);
+    c.v_scale_dev = data<uint8_t>(vs);
+    c.pages = pages;
+    const auto narrow = [](int64_t v) { return static_cast<int>(v > INT32_MAX ? INT32_MAX : v); };      // (refused by the library either way)
+    c.heads = narrow(heads);
+    c.page_size = narrow(page);
+    c.D = narrow(D);
+    return c;
+}
+
+// (k_codes, k_scale, v_codes, v_scale, k, v, slots, positions, table, interleaved, q, q_out)
+PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Tensors a(args, n, 12);
+    const apnn_kv_cache c = read_cache(a);
+    const at::Tensor *k = a.strided("k", 3), *v = a.strided("v", 3), *slots = a.dense("slots", 1, at::kLong);
+    const at::Tensor *positions = a.dense("positions", 1, at::kInt, true), *table = a.dense("table", 2, at::kFloat, true);
+    const long long interleaved = a.integer();
+    const at::Tensor *q = a.strided("q", 3, true), *q_out = a.strided("q_out", 3, true);
+    apnn_kv_tokens t = {};
+    t.type = a.type("k", k);
+    a.same_type("v", v, k);
+    a.same_type("q", q, k);
+    a.same_type("q_out", q_out, k);
+    if (!a.ok()) return nullptr;
+    t.tokens = k->size(0);
+    a.sizes("k", k, {t.tokens, c.heads, c.D});
+    a.sizes("v", v, {t.tokens, c.heads, c.D});
+    a.sizes("slots", slots, {t.tokens});
+    a.sizes("positions", positions, {t.tokens});
+    if (!q != !q_out || !table != !positions) a.fail(PyExc_ValueError, "q goes with q_out, and positions with a table");
+    if (q) {
+        a.sizes("q", q, {t.tokens, q->size(1), c.D});
+        a.sizes("q_out", q_out, {t.tokens, q->size(1), c.D});
+    }
+    if (!a.ok()) return nullptr;
+    t.k_dev = data<void>(k);
+    t.v_dev = data<void>(v);
+    t.k_token_stride = k->stride(0); t.k_head_stride = k->stride(1);
+    t.v_token_stride = v->stride(0); t.v_head_stride = v->stride(1);
+    t.slot_dev = data<int64_t>(slots);
+    if (table) {
+        t.rot = static_cast<int>(table->size(1) > INT32_MAX ? INT32_MAX : table->size(1));
+        t.interleaved = interleaved != 0;
+        t.table_dev = data<float>(table);
+        t.table_rows = table->size(0);
+        t.position_dev = data<int32_t>(positions);
+    }
+    if (q && q->size(1)) {
+        t.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
+        t.q_dev = data<void>(q);
+        t.q_out_dev = data<void>(q_out);
+        t.q_token_stride = q->stride(0); t.q_head_stride = q->stride(1);
+        t.q_out_token_stride = q_out->stride(0); t.q_out_head_stride = q_out->stride(1);
+    }
+    return a.call([&](void *st) { return apnn_kv_append(&c, &t, st); });
+}
+
+PyObject *py_kv_read(PyObject *, PyObject *const *args, Py_ssize_t n)           // (k_codes, k_scale, v_codes, v_scale, slots, k_out, v_out)
+{
+    Tensors a(args, n, 7);
+    const apnn_kv_cache c = read_cache(a);
+    const at::Tensor *slots = a.dense("slots", 1, at::kLong), *k = a.strided("k_out", 3, true), *v = a.strided("v_out", 3, true);
+    const apnn_dtype type = a.type("k_out", k ? k : v);
+    a.same_type("v_out", v, k);
+    if (!a.ok()) return nullptr;
+    const int64_t count = slots->size(0);
+    a.sizes("k_out", k, {count, c.heads, c.D});
+    a.sizes("v_out", v, {count, c.heads, c.D});
+    if (a.ok() && ((k && !k->is_contiguous()) || (v && !v->is_contiguous()))) a.fail(PyExc_AssertionError, "k_out and v_out: contiguous tensors are expected");
+    if (!a.ok()) return nullptr;
+    return a.call([&](void *st) { return apnn_kv_read(&c, data<int64_t>(slots), count, data<void>(k), data<void>(v), type, st); });
+}
+
+// (k_codes, k_scale, v_codes, v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
+PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Tensors a(args, n, 12);
+    const apnn_kv_cache c = read_cache(a);
+    const at::Tensor *q = a.strided("q", 3), *lens = a.dense("lens", 1, at::kInt), *pages = a.dense("pages", 2, at::kInt);
+    apnn_kv_attention_desc d = {};
+    d.scale = a.real();
+    const at::Tensor *q_start = a.dense("q_start", 1, at::kInt, true);
+    d.max_q = a.integer();
+    const at::Tensor *out = a.strided("out", 3), *workspace = a.dense("workspace", 1, at::kByte, true);
+    d.type = a.type("q", q);
+    a.same_type("out", out, q);
+    if (!a.ok()) return nullptr;
+    d.tokens = q->size(0);
+    d.seqs = lens->size(0);
+    d.max_pages = pages->size(1);
+    a.sizes("q", q, {d.tokens, q->size(1), c.D});
+    a.sizes("out", out, {d.tokens, q->size(1), c.D});
+    a.sizes("pages", pages, {d.seqs, d.max_pages});
+    a.sizes("q_start", q_start, {d.seqs + 1});
+    if (!a.ok()) return nullptr;
+    d.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
+    d.q_dev = data<void>(q);
+    d.out_dev = data<void>(out);
+    d.q_token_stride = q->stride(0); d.q_head_stride = q->stride(1);
+    d.out_token_stride = out->stride(0); d.out_head_stride = out->stride(1);
+    d.q_start_dev = data<int32_t>(q_start);
+    d.len_dev = data<int32_t>(lens);
+    d.page_dev = data<int32_t>(pages);
+    at::Tensor own;                                       // of this call: freed on return, in the stream's order
+    void *scratch = data<void>(workspace);
+    size_t bytes = workspace ? static_cast<size_t>(workspace->numel()) : 0;
+    if (!workspace) {
+        bytes = apnn_kv_attention_workspace_bytes(&d, &c);
+        if (bytes) {
+            own = at::empty({static_cast<int64_t>(bytes)}, at::TensorOptions().dtype(at::kByte).device(a.device()));
+            scratch = own.data_ptr();
+        }
+    }
+    return a.call([&](void *st) { return apnn_kv_attention(&d, &c, scratch, bytes, st); });
+}
+
+PyObject *py_kv_attention_workspace(PyObject *, PyObject *const *args, Py_ssize_t n)    // (heads, page_size, D, tokens, q_heads, seqs, max_pages, ragged, max_q)
+{
+    Tensors a(args, n, 9);
+    apnn_kv_cache c = {};
+    apnn_kv_attention_desc d = {};
+    c.heads = static_cast<int>(a.integer());
+    c.page_size = static_cast<int>(a.integer());
+    c.D = static_cast<int>(a.integer());
+    d.tokens = a.integer();
+    d.q_heads = static_cast<int>(a.integer());
+    d.seqs = a.integer();
+    d.max_pages = a.integer();
+    static const int32_t some = 0;
+    d.q_start_dev = a.integer() ? &some : nullptr;        // (whether there is one is all that counts)
+    d.max_q = a.integer();
+    d.type = APNN_F16;
+    if (!a.ok()) return nullptr;
+    const size_t bytes = apnn_kv_attention_workspace_bytes(&d, &c);
+    if (!bytes && apnn_last_error()[0]) return finish(APNN_ERR_INVALID_ARG);
+    return PyLong_FromSize_t(bytes);
+}
+
 // ---- Chain: the library calls of a network in order, recorded once (descriptors and the tensors they were given) and
 // enqueued by one call.  The tensors are held, and their device pointers are checked and taken anew by every pass, so that
 // one whose storage is exchanged is read where it is now, and refused if it now lies on the host or is strided.
@@ -594,6 +899,8 @@ PyMethodDef methods[] = {
     FAST("pack", py_pack), FAST("pack_fmap", py_pack_fmap), FAST("quantize", py_quantize), FAST("gemm", py_gemm),
     FAST("conv2d", py_conv2d), FAST("layer", py_layer), FAST("layer_pair", py_layer_pair), FAST("input_layer", py_input_layer),
     FAST("maxpool", py_maxpool), FAST("sumpool", py_sumpool), FAST("sumpool_fc", py_sumpool_fc), FAST("versions", py_versions),
+    FAST("quantize_tokens", py_quantize_tokens), FAST("gemm_scaled", py_gemm_scaled), FAST("kv_append", py_kv_append), FAST("kv_read", py_kv_read),
+    FAST("kv_attention", py_kv_attention), FAST("kv_attention_workspace", py_kv_attention_workspace),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
