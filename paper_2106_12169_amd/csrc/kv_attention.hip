@@ -15,8 +15,11 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 struct AttentionArgs {
     apnn_kv_attention_desc d;
     apnn_kv_cache c;
-    int page_shift, group;                                // query heads to a cache head
+    float *parts;                                         // workspace
     int64_t tiles;                                        // 16-row tiles of max_q * group rows
+    int page_shift, group;                                // query heads to a cache head
+    int splits, part_rows;                                // of a tile's tokens; rows of a tile that there can be
+    bool q_aligned;                                       // queries can be read 16 bytes at a time
 };
 
 // 16-bit operand types of the scores
@@ -53,18 +56,90 @@ template <class T> __device__ __forceinline__ u32x4_t values8(uint32_t w, float 
 // A row's scale as the conversions take it; 255 stands for NaN there too.
 __device__ __forceinline__ float unit_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Geometry of a lane's share of a row: lane l of a wave has token l % 16 of 16 and channels [D / 4 * (l / 16), + D / 4).
+// A lane's share of a row: lane l of a wave has token l % 16 of 16 and channels [D / 4 * (l / 16), + D / 4).
 template <int D> struct Share {
     static constexpr int words = D / 32;                  // 32-bit words of codes
     static constexpr int units = D == 96 || D == 256 ? 2 : 1;             // groups of 32 channels it reaches into
     static __device__ __forceinline__ int unit(int quarter, int word) { return (quarter * (D / 4) + 8 * word) / 32 - quarter * (D / 4) / 32; }
 };
+template <int D> struct Codes { uint32_t w[Share<D>::words]; };
+
+// Keys and values of 32 tokens as they lie in the cache.
+template <int D> struct Fetched {
+    Codes<D> k[2], v[2];
+    uint8_t ku[2][Share<D>::units], vu[2][Share<D>::units];
+    bool there[2];                                        // the page of these 16 tokens is one of the cache
+};
 
 // Bytes between rows of values in LDS: 32 more than the values, so that eight rows cover all banks.
 template <int D> constexpr int kValueRow = 2 * D + 32;
 
-// 16 query rows of one cache head against the sequence, the four waves taking 32 tokens each in turn.
-template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_kernel(AttentionArgs a, int64_t first)
+// Over the four lanes that share a column (lane ^ 16, lane ^ 32).
+__device__ __forceinline__ float column_max(float x)
+{
+    typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+    u32x2_t y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
+// What a block works on: 16 rows (queries x the heads that share a cache head, heads inside) of one sequence and cache head.
+struct Rows {
+    int64_t q0;                                           // first query row of the sequence
+    int n, all, have;                                     // its queries, at most max_q of them and all; its tokens that the table can name
+    int shift;                                            // query i sees have' = min(have, shift + i + 1) tokens
+    int r0;                                               // first row of the tile
+    int most;                                             // tokens that any of the 16 rows sees
+    bool any;
+};
+
+__device__ __forceinline__ int seen_by(const Rows &x, int i) { return min(max(x.shift + i + 1, 0), x.have); }
+
+__device__ __forceinline__ Rows find_rows(const AttentionArgs &a, int64_t b, int64_t tile)
+{
+    Rows x = {};
+    int64_t n = 1;
+    x.q0 = b;
+    if (a.d.q_start_dev) {
+        x.q0 = a.d.q_start_dev[b];
+        n = a.d.q_start_dev[b + 1] - x.q0;
+    }
+    if (x.q0 < 0 || x.q0 > a.d.tokens) return x;
+    n = n < a.d.tokens - x.q0 ? n : a.d.tokens - x.q0;
+    x.all = static_cast<int>(n);
+    x.n = static_cast<int>(n < a.d.max_q ? n : a.d.max_q);
+    if (tile * 16 >= int64_t(x.n) * a.group) return x;
+    x.any = true;
+    x.r0 = static_cast<int>(tile * 16);
+    const int len = a.d.len_dev[b], room = static_cast<int>(a.d.max_pages << a.page_shift);
+    x.have = min(max(len, 0), room);
+    x.shift = max(len, 0) - x.all;
+    const int last = min((x.r0 + 15) / a.group, x.n - 1);
+    x.most = seen_by(x, last);
+    return x;
+}
+
+// Tokens of a split: a tile's tokens over `splits`, whole turns of the block's waves, and no fewer than pay for the joining.
+constexpr int kTurn = 128, kLeastSplit = 256;
+__host__ __device__ __forceinline__ int split_tokens(int most, int splits)
+{
+    const int each = ((most + splits - 1) / splits + kTurn - 1) / kTurn * kTurn;
+    return each < kLeastSplit ? kLeastSplit : each;
+}
+
+// Parts of a tile's rows in the workspace: [tile of tiles x heads x seqs][split][row] of D sums, then maximum and sum of weights.
+template <int D> __device__ __forceinline__ float *part_of(const AttentionArgs &a, int64_t unit, int split, int row)
+{
+    return a.parts + ((unit * a.splits + split) * a.part_rows + row) * (D + 4);
+}
+
+// 16 query rows of one cache head against one split of the sequence, the four waves taking 32 tokens each in turn.
+//
+// Bound by memory: (D / 2 + D / 32) 2 bytes a token and cache head.  A wave has the next 32 tokens' codes in flight, in
+// registers, while it works on the current ones, and the page numbers of the 32 after those; four blocks of four waves fit
+// a compute unit, 70 KB in flight.  LDS is only the way V is transposed, private to a wave: no barrier before the end.
+template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 2 : 4) void kv_attention_kernel(AttentionArgs a, int64_t first)
 {
     using Op = Operand<T>;
     constexpr int steps = D / 32, tokens = 32;
@@ -72,98 +147,104 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_ke
     __shared__ alignas(16) char lds[4][wave_bytes];
     __shared__ float row_max[4][16], row_sum[4][16];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, quarter = lane >> 4;
-    const int64_t id = first + blockIdx.x, tile = id % a.tiles, rest = id / a.tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, quarter = lane >> 4;
+    int64_t id = first + blockIdx.x;
+    const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
+    const int64_t unit = SPLIT ? id / a.splits : id, tile = unit % a.tiles, rest = unit / a.tiles;
     const int head = static_cast<int>(rest % a.c.heads);
     const int64_t b = rest / a.c.heads;
     if (b >= a.d.seqs) return;
-
-    // the sequence: rows [q0, q0 + n), `have` tokens that the table can name
-    int64_t q0 = b, n = 1;
-    if (a.d.q_start_dev) {
-        q0 = a.d.q_start_dev[b];
-        n = a.d.q_start_dev[b + 1] - q0;
+    const Rows x = find_rows(a, b, tile);
+    if (!x.any) return;
+    int begin = 0, end = x.most;
+    if (SPLIT) {
+        const int each = split_tokens(x.most, a.splits);
+        if (split && static_cast<int64_t>(split) * each >= x.most) return;
+        begin = split * each;
+        end = min(begin + each, x.most);
     }
-    if (q0 < 0 || q0 > a.d.tokens) return;
-    n = n < a.d.tokens - q0 ? n : a.d.tokens - q0;
-    const int64_t all = n;                                // where the queries stand goes by all of them
-    n = n < a.d.max_q ? n : a.d.max_q;
-    const int64_t r0 = tile * 16;
-    if (r0 >= n * a.group) return;
-    const int64_t len = a.d.len_dev[b], room = a.d.max_pages << a.page_shift;
-    const int64_t have = len < room ? (len > 0 ? len : 0) : room;
 
-    const int64_t r = r0 + c, i = r / a.group;
-    const bool live = i < n;
-    const int64_t at = (live ? i : 0) + q0;
-    const int qh = head * a.group + static_cast<int>(r - i * a.group);
-    // tokens that the row of this lane's column sees, and the most any row of the tile sees
-    int64_t seen = len - all + i + 1;
-    seen = !live || seen < 0 ? 0 : (seen < have ? seen : have);
-    const int64_t last = r0 + 15 < n * a.group ? (r0 + 15) / a.group : n - 1;
-    int64_t most = len - all + last + 1;
-    most = most < 0 ? 0 : (most < have ? most : have);
-
+    const int r = x.r0 + c, i = r / a.group;
+    const bool live = i < x.n;
+    const int seen = live ? seen_by(x, i) : 0;
     typename Op::vec q[steps];
     {
-        const T *src = static_cast<const T *>(a.d.q_dev) + at * a.d.q_token_stride + (live ? qh : head * a.group) * a.d.q_head_stride + quarter * (D / 4);
+        const int qh = head * a.group + (live ? r - i * a.group : 0);
+        const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + quarter * (D / 4);
+        if (a.q_aligned) {
 #pragma unroll
-        for (int s = 0; s < steps; ++s)
+            for (int s = 0; s < steps; ++s) q[s] = *reinterpret_cast<const typename Op::vec *>(src + 8 * s);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[s][j] = src[8 * s + j];
+            for (int s = 0; s < steps; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[s][j] = src[8 * s + j];
+        }
     }
     const float factor = a.d.scale * 1.4426950408889634f; // scores in powers of two
     const int32_t *pages = a.d.page_dev + b * a.d.max_pages;
     char *const mine = lds[wave];
+    const uint32_t code_at = c * (D / 2) + quarter * (D / 8), unit_at = c * (D / 32) + quarter * (D / 4) / 32;
+    const int mask = (1 << a.page_shift) - 1;
+
+    const auto page_of = [&](int t) { return pages[t < end ? t >> a.page_shift : 0]; };      // (there is a first page if there are tokens)
+    const auto fetch = [&](int t0, const int (&page)[2]) {
+        Fetched<D> f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int t = t0 + 16 * u;
+            f.there[u] = t < end && page[u] >= 0 && page[u] < a.c.pages;
+            const int64_t row = ((static_cast<int64_t>(f.there[u] ? page[u] : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
+            f.k[u] = *reinterpret_cast<const Codes<D> *>(a.c.k_codes_dev + row * (D / 2) + code_at);
+            f.v[u] = *reinterpret_cast<const Codes<D> *>(a.c.v_codes_dev + row * (D / 2) + code_at);
+#pragma unroll
+            for (int y = 0; y < Share<D>::units; ++y) {
+                const uint32_t at = unit_at + (y ? Share<D>::unit(quarter, steps - 1) : 0);    // (the second group of a 96-channel share may be the first again)
+                f.ku[u][y] = (a.c.k_scale_dev + row * (D / 32))[at];
+                f.vu[u][y] = (a.c.v_scale_dev + row * (D / 32))[at];
+            }
+        }
+        return f;
+    };
 
     f32x4_t out[D / 16] = {};
     float top = -INFINITY, sum = 0.0f;                    // of this lane's column: common to its four lanes, and this lane's part
-    for (int64_t t0 = wave * tokens; t0 < most; t0 += 4 * tokens) {
-        f32x4_t score[2];
+    int t0 = begin + wave * tokens;
+    int page[2] = {};
+    Fetched<D> now = {};
+    if (t0 < end) {
+        page[0] = page_of(t0);
+        page[1] = page_of(t0 + 16);
+        now = fetch(t0, page);
+        page[0] = page_of(t0 + kTurn);
+        page[1] = page_of(t0 + kTurn + 16);
+    }
+    for (; t0 < end; t0 += kTurn) {
+        const Fetched<D> next = fetch(t0 + kTurn, page);
+        page[0] = page_of(t0 + 2 * kTurn);
+        page[1] = page_of(t0 + 2 * kTurn + 16);
+        f32x4_t score[2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int64_t t = t0 + 16 * u;
-            const int64_t page = t < most ? __builtin_amdgcn_readfirstlane(pages[t >> a.page_shift]) : -1;
-            const bool there = page >= 0 && page < a.c.pages;
-            const int64_t row = there ? ((page * a.c.heads + head) << a.page_shift) + (t & ((1 << a.page_shift) - 1)) + c : 0;
-            uint32_t kw[steps] = {}, vw[steps] = {}, ku[Share<D>::units], vu[Share<D>::units];
-#pragma unroll
-            for (int x = 0; x < Share<D>::units; ++x) ku[x] = vu[x] = 127;
-            if (there) {
-#pragma unroll
-                for (int s = 0; s < steps; ++s) {
-                    kw[s] = reinterpret_cast<const uint32_t *>(a.c.k_codes_dev + row * (D / 2))[quarter * steps + s];
-                    vw[s] = reinterpret_cast<const uint32_t *>(a.c.v_codes_dev + row * (D / 2))[quarter * steps + s];
-                }
-                const int64_t at_scale = row * (D / 32) + quarter * (D / 4) / 32;
-#pragma unroll
-                for (int x = 0; x < Share<D>::units; ++x) {
-                    // (the second group of a 96-channel share may be the first again)
-                    const int64_t where = at_scale + (x ? Share<D>::unit(quarter, steps - 1) : 0);
-                    ku[x] = a.c.k_scale_dev[where];
-                    vu[x] = t + c < have ? a.c.v_scale_dev[where] : 127;       // beyond the end: whatever it is, finite
-                }
-            }
-            score[u] = f32x4_t{};
+            const bool written = now.there[u] && t0 + 16 * u + c < x.have;     // beyond the end: whatever it is, made finite
 #pragma unroll
             for (int s = 0; s < steps; ++s) {
-                const int x = Share<D>::units > 1 ? Share<D>::unit(quarter, s) : 0;
-                const u32x4_t k = values8<T>(kw[s], unit_of(x ? ku[Share<D>::units - 1] : ku[0]));
+                const bool second = Share<D>::units > 1 && Share<D>::unit(quarter, s);
+                const u32x4_t k = values8<T>(now.k[u].w[s], unit_of(now.ku[u][second ? Share<D>::units - 1 : 0]));
                 score[u] = Op::product(__builtin_bit_cast(typename Op::vec, k), q[s], score[u]);
-                const u32x4_t v = values8<_Float16>(vw[s], unit_of(x ? vu[Share<D>::units - 1] : vu[0]));
+                const u32x4_t v = values8<_Float16>(now.v[u].w[s], unit_of(written ? now.vu[u][second ? Share<D>::units - 1 : 0] : 127));
                 *reinterpret_cast<u32x4_t *>(mine + (16 * u + c) * kValueRow<D> + (quarter * (D / 4) + 8 * s) * 2) = v;
             }
+            const int limit = now.there[u] ? seen - t0 - 16 * u - 4 * quarter : 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                score[u][j] = there && t + 4 * quarter + j < seen ? score[u][j] * factor : -INFINITY;
+            for (int j = 0; j < 4; ++j) score[u][j] = j < limit ? score[u][j] * factor : -INFINITY;
         }
         float best = top;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int j = 0; j < 4; ++j) best = fmaxf(best, score[u][j]);
-        best = fmaxf(best, __shfl_xor(best, 16));
-        best = fmaxf(best, __shfl_xor(best, 32));
+        best = column_max(best);
         const float base = best == -INFINITY ? 0.0f : best, keep = __builtin_amdgcn_exp2f(top - base);
         top = best;
         half8_t p;
@@ -185,15 +266,15 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_ke
             half8_t v;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4_t *)(from + 16 * u * kValueRow<D>));
+                const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(from + 16 * u * kValueRow<D>));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[4 * u + j] = __builtin_bit_cast(_Float16, static_cast<short>(x[j]));
+                for (int j = 0; j < 4; ++j) v[4 * u + j] = __builtin_bit_cast(_Float16, static_cast<short>(y[j]));
             }
             out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, out[d] * keep, 0, 0, 0);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        now = next;
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -206,10 +287,9 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_ke
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4_t *>(mine + (c * D + ((16 * d + 4 * quarter) ^ (4 * c & 15))) * 4) = out[d];
     __syncthreads();
-    for (int x = threadIdx.x; x < 16 * D / 4; x += 256) {
-        const int row = x / (D / 4), ch = x % (D / 4) * 4;
-        const int64_t rr = r0 + row, ri = rr / a.group;
-        if (ri >= n) continue;
+    for (int y = threadIdx.x; y < 16 * D / 4; y += 256) {
+        const int row = y / (D / 4), ch = y % (D / 4) * 4, rr = x.r0 + row, ri = rr / a.group;
+        if (ri >= x.n) continue;
         float m = row_max[0][row];
         for (int w = 1; w < 4; ++w) m = fmaxf(m, row_max[w][row]);
         const float base = m == -INFINITY ? 0.0f : m;
@@ -220,10 +300,61 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_ke
             l += row_sum[w][row] * f;
             o += *reinterpret_cast<const f32x4_t *>(lds[w] + (row * D + (ch ^ (4 * row & 15))) * 4) * f;
         }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        T *to = static_cast<T *>(a.d.out_dev) + (q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + ch;
-        for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
+        if (SPLIT) {
+            float *part = part_of<D>(a, unit, split, row);
+            *reinterpret_cast<f32x4_t *>(part + ch) = o;
+            if (ch == 0) {
+                part[D] = m;
+                part[D + 1] = l;
+            }
+        } else {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + ch;
+            for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
+        }
     }
+}
+
+// Joins the splits' parts of one row, a block a row: D / 4 lanes take its channels, the others further splits.
+template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a, int64_t first)
+{
+    constexpr int lanes = D / 4, teams = 256 / lanes;
+    __shared__ f32x4_t sums[teams][lanes];
+    __shared__ float weights[teams];
+    const int64_t id = first + blockIdx.x, unit = id / a.part_rows, tile = unit % a.tiles, rest = unit / a.tiles;
+    const int row = static_cast<int>(id - unit * a.part_rows), head = static_cast<int>(rest % a.c.heads);
+    const int64_t b = rest / a.c.heads;
+    if (b >= a.d.seqs) return;
+    const Rows x = find_rows(a, b, tile);
+    const int rr = x.r0 + row, ri = rr / a.group;
+    if (!x.any || ri >= x.n) return;
+    const int each = split_tokens(x.most, a.splits), parts = max(1, (x.most + each - 1) / each);
+    float m = -INFINITY;
+    for (int s = threadIdx.x & 63; s < parts; s += 64) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    const float base = m == -INFINITY ? 0.0f : m;
+    const int team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    float l = 0.0f;
+    f32x4_t o = {};
+    if (team < teams) {
+        for (int s = team; s < parts; s += teams) {
+            const float *part = part_of<D>(a, unit, s, row);
+            const float f = __builtin_amdgcn_exp2f(part[D] - base);
+            l += part[D + 1] * f;
+            o += *reinterpret_cast<const f32x4_t *>(part + 4 * lane) * f;
+        }
+        sums[team][lane] = o;
+        if (lane == 0) weights[team] = l;
+    }
+    __syncthreads();
+    if (team) return;
+    for (int s = 1; s < teams; ++s) {
+        o += sums[s][lane];
+        l += weights[s];
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + 4 * lane;
+    for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
 }
 
 }  // namespace apnn
@@ -241,6 +372,9 @@ int check_attention(const char *who, const apnn_kv_attention_desc *d, const apnn
                     (long long)d->seqs, (long long)d->max_pages, (long long)d->max_q, d->q_heads);
     if (d->tokens > INT_MAX || d->seqs > INT_MAX || d->max_pages > INT_MAX || d->q_heads > (1 << 16))
         return fail(APNN_ERR_UNSUPPORTED, "%s: a size is too large", who);
+    if (d->max_pages * c->page_size > (int64_t(1) << 30)) return fail(APNN_ERR_UNSUPPORTED, "%s: a table of more than 2^30 tokens", who);
+    if (d->q_heads >= c->heads && d->tokens * (d->q_heads / c->heads) > (int64_t(1) << 30))
+        return fail(APNN_ERR_UNSUPPORTED, "%s: %lld rows of %d heads for each cache head", who, (long long)d->tokens, d->q_heads / c->heads);
     if (d->q_heads < 1 || d->q_heads % c->heads) return fail(APNN_ERR_INVALID_ARG, "%s: %d query heads over %d cache heads", who, d->q_heads, c->heads);
     if (!(d->scale - d->scale == 0.0f)) return fail(APNN_ERR_INVALID_ARG, "%s: scale is not finite", who);
     if (!d->q_start_dev && d->tokens < d->seqs) return fail(APNN_ERR_INVALID_ARG, "%s: one query each for %lld sequences, %lld rows", who, (long long)d->seqs, (long long)d->tokens);
@@ -249,11 +383,39 @@ int check_attention(const char *who, const apnn_kv_attention_desc *d, const apnn
 
 }  // namespace
 
+namespace apnn {
+
+// How a call is cut: 16-row tiles, and splits of their tokens where tiles are too few to fill the chip.  A compute unit holds
+// four blocks; twice as many blocks as that leave room for sequences of different lengths.
+struct AttentionPlan {
+    int64_t max_q, tiles;
+    int splits, part_rows;
+    size_t bytes;
+};
+
+static AttentionPlan plan_attention(const apnn_kv_attention_desc &d, const apnn_kv_cache &c)
+{
+    AttentionPlan p = {};
+    const int group = d.q_heads / c.heads;
+    p.max_q = d.q_start_dev ? (d.max_q < d.tokens ? d.max_q : d.tokens) : 1;
+    if (d.tokens == 0 || d.seqs == 0 || p.max_q == 0) return p;
+    p.tiles = ceil_div(p.max_q * group, 16);
+    p.part_rows = static_cast<int>(p.max_q * group < 16 ? p.max_q * group : 16);
+    const int64_t blocks = p.tiles * c.heads * d.seqs, room = d.max_pages * c.page_size;
+    int64_t splits = ceil_div(2048, blocks);
+    if (splits > ceil_div(room, kLeastSplit)) splits = ceil_div(room, kLeastSplit);
+    p.splits = splits < 1 ? 1 : static_cast<int>(splits);
+    if (p.splits > 1) p.bytes = static_cast<size_t>(blocks) * p.splits * p.part_rows * (c.D + 4) * sizeof(float);
+    return p;
+}
+
+}  // namespace apnn
+
 extern "C" size_t apnn_kv_attention_workspace_bytes(const apnn_kv_attention_desc *desc, const apnn_kv_cache *cache)
 {
     apnn::clear_error();
     if (check_attention("apnn_kv_attention_workspace_bytes", desc, cache) != APNN_OK) return 0;
-    return 0;
+    return apnn::plan_attention(*desc, *cache).bytes;
 }
 
 extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_kv_cache *cache, void *workspace_dev, size_t workspace_bytes, void *stream)
@@ -262,24 +424,42 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
     clear_error();
     const char *who = "apnn_kv_attention";
     if (const int rc = check_attention(who, desc, cache)) return rc;
-    const int64_t max_q = desc->q_start_dev ? (desc->max_q < desc->tokens ? desc->max_q : desc->tokens) : 1;
-    if (desc->tokens == 0 || desc->seqs == 0 || max_q == 0) return APNN_OK;
+    const AttentionPlan plan = plan_attention(*desc, *cache);
+    if (plan.tiles == 0) return APNN_OK;
     if (!desc->q_dev || !desc->out_dev || !desc->len_dev || (desc->max_pages && !desc->page_dev)) return fail(APNN_ERR_INVALID_ARG, "%s: null pointer", who);
     if (!aligned_to(desc->q_dev, desc->type) || !aligned_to(desc->out_dev, desc->type)) return fail(APNN_ERR_ALIGNMENT, "%s: a pointer is not aligned to its type", who);
     if (!strides_fit(desc->tokens, desc->q_heads, cache->D, desc->q_token_stride, desc->q_head_stride, false) ||
         !strides_fit(desc->tokens, desc->q_heads, cache->D, desc->out_token_stride, desc->out_head_stride, true))
         return fail(APNN_ERR_INVALID_ARG, "%s: strides", who);
-    (void)workspace_dev;
-    (void)workspace_bytes;
-    AttentionArgs a = {*desc, *cache, shift_of(cache->page_size), desc->q_heads / cache->heads, 0};
-    a.d.max_q = max_q;
-    a.tiles = ceil_div(max_q * a.group, 16);
-    const int64_t blocks = a.tiles * cache->heads * desc->seqs;
+    if (plan.bytes && (!workspace_dev || workspace_bytes < plan.bytes))
+        return fail(APNN_ERR_INVALID_ARG, "%s: a workspace of %zu bytes is needed, %zu given", who, plan.bytes, workspace_dev ? workspace_bytes : size_t(0));
+    if (plan.bytes && !aligned16(workspace_dev)) return fail(APNN_ERR_ALIGNMENT, "%s: the workspace is not 16-byte aligned", who);
+    AttentionArgs a = {};
+    a.d = *desc;
+    a.c = *cache;
+    a.d.max_q = plan.max_q;
+    if (cache->pages == 0) a.d.max_pages = 0;             // no page can be read
+    a.parts = static_cast<float *>(workspace_dev);
+    a.tiles = plan.tiles;
+    a.page_shift = shift_of(cache->page_size);
+    a.group = desc->q_heads / cache->heads;
+    a.splits = plan.splits;
+    a.part_rows = plan.part_rows;
+    a.q_aligned = aligned16(desc->q_dev) && desc->q_token_stride % 8 == 0 && desc->q_head_stride % 8 == 0;
+    const int64_t units = a.tiles * cache->heads * desc->seqs;
+    const auto sliced = [](int64_t blocks, auto &&launch) {
+        for (int64_t first = 0; first < blocks; first += kMaxBlocks) launch(first, static_cast<unsigned>(blocks - first < kMaxBlocks ? blocks - first : kMaxBlocks));
+    };
     const auto go = [&](auto t, auto d) {
-        for (int64_t first = 0; first < blocks; first += kMaxBlocks)
-            kv_attention_kernel<decltype(t), decltype(d)::value><<<static_cast<unsigned>(blocks - first < kMaxBlocks ? blocks - first : kMaxBlocks), 256, 0, as_stream(stream)>>>(a, first);
+        using T = decltype(t);
+        constexpr int D = decltype(d)::value;
+        if (a.splits == 1) {
+            sliced(units, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, false><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
+        } else {
+            sliced(units * a.splits, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
+            sliced(units * a.part_rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
+        }
         return check_launch(who);
     };
-    const auto of_type = [&](auto d) { return desc->type == APNN_F16 ? go(_Float16{}, d) : go(__bf16{}, d); };
-    return by_channels(cache->D, of_type);
+    return by_channels(cache->D, [&](auto d) { return desc->type == APNN_F16 ? go(_Float16{}, d) : go(__bf16{}, d); });
 }
