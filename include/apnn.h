@@ -284,7 +284,8 @@ int apnn_quantize_tokens(const void *src_dev, apnn_dtype type, int64_t rows, int
                          int8_t *codes_dev, float *scale_dev, void *stream);
 
 /* Y[m][n] = x_scale[m] * w_scale[n] * sum_k X[m][k] W[n][k] + bias[n], the sum in
- * int32 (exact), the rest in 64 bits, rounded to the result's type.
+ * int32 (exact), scaled in fp32 without intermediates that overflow or vanish (three
+ * roundings before the bias), then rounded to the result's type.
  * X_dev: int8 [M][pitch], W_dev: int8 [N][pitch], pitch = apnn_token_pitch(K), both
  * 16-byte aligned, bytes K and up of a row 0; any int8 code, -128 among them.
  * bias_dev: fp32 [N] or NULL.  Y_dev: row m starts ldy elements (>= N) after row
