@@ -43,4 +43,27 @@ template <class T> struct alignas(16) Pack16 {
     T v[n];
 };
 
+// Eight neighbouring elements as fp32, whatever their alignment (one or two 16-byte loads).
+template <class T> __device__ __forceinline__ void load8(const T *from, float (&to)[8])
+{
+    T raw[8];
+    __builtin_memcpy(raw, from, sizeof raw);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[j] = static_cast<float>(raw[j]);
+}
+template <class T> __device__ __forceinline__ void store8(const float (&from)[8], T *to)
+{
+    T raw[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) raw[j] = static_cast<T>(from[j]);
+    __builtin_memcpy(to, raw, sizeof raw);
+}
+
+// n / d for 0 <= n, 0 < d: in 32 bits where they do, which takes a third of the instructions.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d)
+{
+    if (((n | d) >> 32) == 0) return static_cast<uint32_t>(n) / static_cast<uint32_t>(d);
+    return n / d;
+}
+
 }  // namespace apnn

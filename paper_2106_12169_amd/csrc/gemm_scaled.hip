@@ -166,9 +166,9 @@ template <class T, int F> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void
 
 // Few tokens: 16 MT tokens x 16 NT channels a block, the block's waves sharing K in turns of 256 bytes.
 //
-// Bound by reading W once.  Lanes load fragments straight from memory, eight (16 NT rows x 64 bytes) loads in flight a wave;
-// a lane's share of a turn is 64 bytes of a row, so every fetched line is used whole (the order of K within a turn is free, the
-// same for both operands).  X comes from L2 again for each block: MT / NT bytes for each byte of W.
+// Bound by reading W once.  Lanes load fragments straight from memory, a load of 16 rows taking 64 neighbouring bytes of each
+// and the four loads of a turn 256 (the order of K within a turn is free, the same for both operands).  The next turn is in
+// flight while one is multiplied.  X comes from L2 again for each block: MT / NT bytes for each byte of W.
 template <class T, int MT, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES) void gemm_scaled_few_kernel(ScaledGemm p)
 {
     constexpr int TURN = 256;
@@ -177,30 +177,46 @@ template <class T, int MT, int NT, int WAVES> __global__ __launch_bounds__(64 * 
     const int n0 = static_cast<int>(blockIdx.x) % p.across * 16 * NT, m0 = static_cast<int>(blockIdx.x) / p.across * 16 * MT;
     const int8_t *w[NT], *x[MT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) w[i] = p.W + static_cast<int64_t>(min(n0 + 16 * i + r, p.N - 1)) * p.pitch + 64 * quarter;
+    for (int i = 0; i < NT; ++i) w[i] = p.W + static_cast<int64_t>(min(n0 + 16 * i + r, p.N - 1)) * p.pitch + 16 * quarter;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) x[i] = p.X + static_cast<int64_t>(min(m0 + 16 * i + r, p.M - 1)) * p.pitch + 64 * quarter;
+    for (int i = 0; i < MT; ++i) x[i] = p.X + static_cast<int64_t>(min(m0 + 16 * i + r, p.M - 1)) * p.pitch + 16 * quarter;
     i32x4_t acc[NT][MT] = {};
-    const auto turn = [&](int k, auto whole) {
-        i32x4_t a[4][NT], b[4][MT];
+    struct Turn { i32x4_t a[4][NT], b[4][MT]; };
+    const auto fetch = [&](int k) {
+        Turn t;
+        const bool whole = k + TURN <= p.pitch;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const bool in = decltype(whole)::value || k + 64 * quarter + 16 * j < p.pitch;
+            const bool in = whole || k + 16 * quarter + 64 * j < p.pitch;
+            const int at = in ? k + 64 * j : -16 * quarter;            // (beyond the end: the row's first bytes, for nothing)
 #pragma unroll
-            for (int i = 0; i < NT; ++i) a[j][i] = in ? *reinterpret_cast<const i32x4_t *>(w[i] + k + 16 * j) : i32x4_t{};
+            for (int i = 0; i < NT; ++i) {
+                t.a[j][i] = *reinterpret_cast<const i32x4_t *>(w[i] + at);
+                if (!in) t.a[j][i] = i32x4_t{};
+            }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) b[j][i] = in ? *reinterpret_cast<const i32x4_t *>(x[i] + k + 16 * j) : i32x4_t{};
+            for (int i = 0; i < MT; ++i) t.b[j][i] = *reinterpret_cast<const i32x4_t *>(x[i] + at);
         }
+        return t;
+    };
+    const auto multiply = [&](const Turn &t) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int l = 0; l < MT; ++l) acc[i][l] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j][i], b[j][l], acc[i][l], 0, 0, 0);
+                for (int l = 0; l < MT; ++l) acc[i][l] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.a[j][i], t.b[j][l], acc[i][l], 0, 0, 0);
     };
     int k = wave * TURN;
-    for (; k + TURN <= p.pitch; k += WAVES * TURN) turn(k, std::true_type{});
-    if (k < p.pitch) turn(k, std::false_type{});
+    if (k < p.pitch) {
+        Turn now = fetch(k);
+        for (k += WAVES * TURN; k < p.pitch; k += WAVES * TURN) {
+            const Turn next = fetch(k);
+            multiply(now);
+            now = next;
+        }
+        multiply(now);
+    }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll

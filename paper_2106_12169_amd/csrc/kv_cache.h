@@ -12,7 +12,7 @@ int check_cache(const char *who, const apnn_kv_cache *c);
 // Row of (token slot, head) in the code and scale arrays.
 __host__ __device__ __forceinline__ int64_t cache_row(int64_t slot, int head, int heads, int page_shift)
 {
-    return ((slot >> page_shift) * heads + head << page_shift) + (slot & ((1 << page_shift) - 1));
+    return (((slot >> page_shift) * heads + head) << page_shift) + (slot & ((1 << page_shift) - 1));
 }
 
 // f(integral constant D) for the supported sizes

@@ -28,20 +28,47 @@ struct AppendArgs {
     int page_shift;
 };
 
+// (a, b) turned: a cos - b sin, b cos + a sin, in 64 bits, rounded once.
+__device__ __forceinline__ void turn(float &a, float &b, float cs, float sn)
+{
+    const double x = a, y = b, c = cs, s = sn;
+    a = static_cast<float>(x * c - y * s);
+    b = static_cast<float>(y * c + x * s);
+}
+
 // Channels c0 .. c0 + 7 of a row, rotated where the rotation reaches them.
 template <class T> __device__ __forceinline__ void rotated8(const T *x, int c0, int rot, bool interleaved, const float *angles, float (&y)[8])
 {
+    load8(x + c0, y);
+    if (c0 >= rot) return;
     const int half = rot >> 1;
+    if (interleaved) {                                    // four pairs, some of them perhaps beyond the rotation
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = c0 + j;
-        y[j] = static_cast<float>(x[c]);
-        if (c < rot) {
-            const int i = interleaved ? c >> 1 : (c < half ? c : c - half);
-            const bool first = interleaved ? !(c & 1) : c < half;
-            const int other = interleaved ? c ^ 1 : (first ? c + half : c - half);
-            const double own = y[j], pair = static_cast<float>(x[other]), cs = angles[i], sn = angles[half + i];
-            y[j] = static_cast<float>(first ? own * cs - pair * sn : own * cs + pair * sn);
+        for (int j = 0; j < 4; ++j) {
+            const int i = (c0 >> 1) + j;
+            if (i < half) turn(y[2 * j], y[2 * j + 1], angles[i], angles[half + i]);
+        }
+    } else if (half % 8 == 0) {                           // the pairs' other halves are eight channels in a row, too
+        float z[8], cs[8], sn[8];
+        const bool first = c0 < half;
+        const int i = first ? c0 : c0 - half;
+        load8(x + (first ? c0 + half : i), z);
+        load8(angles + i, cs);
+        load8(angles + half + i, sn);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float a = first ? y[j] : z[j], b = first ? z[j] : y[j];
+            turn(a, b, cs[j], sn[j]);
+            y[j] = first ? a : b;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = c0 + j, i = c < half ? c : c - half;
+            if (c >= rot) continue;
+            float a = c < half ? y[j] : static_cast<float>(x[i]), b = c < half ? static_cast<float>(x[c + half]) : y[j];
+            turn(a, b, angles[i], angles[half + i]);
+            y[j] = c < half ? a : b;
         }
     }
 }
@@ -80,7 +107,7 @@ template <class T, int D, int TEAM> __global__ __launch_bounds__(256) void kv_ap
 {
     const int64_t item = first + static_cast<int64_t>(blockIdx.x) * (256 / TEAM) + threadIdx.x / TEAM;
     const int heads = a.c.heads + a.t.q_heads, part = threadIdx.x % TEAM, c0 = part * 8;
-    const int64_t token = item / heads;
+    const int64_t token = quotient(item, heads);
     const int h = static_cast<int>(item - token * heads);
     bool live = token < a.t.tokens && c0 < D;
     int64_t slot = 0;
@@ -102,16 +129,13 @@ template <class T, int D, int TEAM> __global__ __launch_bounds__(256) void kv_ap
         rotated8(q, c0, a.t.rot, a.t.interleaved, angles, y);
         T *out = static_cast<T *>(a.t.q_out_dev) + token * a.t.q_out_token_stride + hq * a.t.q_out_head_stride + c0;
         __builtin_amdgcn_wave_barrier();                  // in place: every lane of the team has read its pairs
-#pragma unroll
-        for (int j = 0; j < 8; ++j) out[j] = static_cast<T>(y[j]);
+        store8(y, out);
         return;
     }
     float z[8] = {};
     if (live) {
         rotated8(static_cast<const T *>(a.t.k_dev) + token * a.t.k_token_stride + h * a.t.k_head_stride, c0, a.t.rot, a.t.interleaved, angles, y);
-        const T *v = static_cast<const T *>(a.t.v_dev) + token * a.t.v_token_stride + h * a.t.v_head_stride + c0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = static_cast<float>(v[j]);
+        load8(static_cast<const T *>(a.t.v_dev) + token * a.t.v_token_stride + h * a.t.v_head_stride + c0, z);
     }
     int bad = !(finite8(y) && finite8(z));
     for (int d = 1; d < TEAM; d <<= 1) bad |= __shfl_xor(bad, d);
@@ -141,9 +165,9 @@ struct ReadArgs {
 // 8 channels of a key row and of a value row a thread.
 template <class T, int D> __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a, int64_t first)
 {
-    const int64_t item = first + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, line = item / (D / 8);
+    const int64_t item = first + static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, line = quotient(item, D / 8);
     const int part = static_cast<int>(item - line * (D / 8));
-    const int64_t at = line / a.c.heads;
+    const int64_t at = quotient(line, a.c.heads);
     if (at >= a.n) return;
     const int64_t slot = a.slot[at];
     const bool there = slot >= 0 && slot < a.c.pages << a.page_shift;
@@ -160,17 +184,15 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_read_kernel(
             if (key_scale == 255) byte = 255;
         }
         const float unit = __uint_as_float(byte == 255 ? 0x7FC00000u : byte << 23);
-        alignas(16) T y[8];
+        float y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t code = w >> (4 * j), low = code & 7;
             // magnitudes in halves: 0 1 2 3 4 6 8 12
             const float half = static_cast<float>(low < 4 ? low : (low < 6 ? 2 * low - 4 : 4 * low - 16));
-            y[j] = static_cast<T>((code & 8 ? -0.5f : 0.5f) * half * unit);
+            y[j] = (code & 8 ? -0.5f : 0.5f) * half * unit;
         }
-        Pack16<T> *to = reinterpret_cast<Pack16<T> *>(out + line * D + part * 8);
-        const Pack16<T> *from = reinterpret_cast<const Pack16<T> *>(y);
-        for (int j = 0; j < 8 / Pack16<T>::n; ++j) to[j] = from[j];
+        store8(y, out + line * D + part * 8);
     }
 }
 
