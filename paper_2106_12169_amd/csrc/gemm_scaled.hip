@@ -4,7 +4,6 @@
 //
 // The sum is exact in int32 (K 2^14 < 2^31 is checked).  It is scaled in fp32 by the scales' mantissas and then by the sum
 // of their exponents, so that no intermediate overflows or vanishes: four roundings of 2^-24 before the result's own.
-// Both kernels take W as the matrix instruction's rows: a lane then ends with neighbouring channels of one token.
 #include "dense.h"
 #include "lane_util.h"
 #include "lds_load.h"
@@ -22,7 +21,6 @@ struct ScaledGemm {
     int64_t ldy;
     int M, N, pitch;                                      // pitch: bytes of a row of X and W
     int across, tiles;                                    // tiles of a row of tiles, of the result
-    bool wide;                                            // rows of Y can be written 16 bytes at a time
 };
 
 struct Scale {
@@ -46,41 +44,46 @@ __device__ __forceinline__ void tile_of(const ScaledGemm &p, int id, int &tm, in
     tn = in / rows;
 }
 
-// 64 F x 64 F outputs a block, 32 F x 32 F a wave, K in chunks of 128 bytes, two of them in LDS.
+// 64 F x 64 F outputs a block, 32 F x 32 F a wave, K in chunks of 128 bytes, STAGES of them in LDS.
 //
 // Bound by the matrix unit (F = 4: 256 accumulators, one wave a SIMD).  A chunk is loaded straight to LDS while the one
 // before it is multiplied, its 16-byte pieces swizzled by row so that fragment reads meet no bank twice; the fragments of a
 // step are read while the step before it is multiplied, one read or load behind each matrix instruction.
-template <class T, int F> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void gemm_scaled_tile_kernel(ScaledGemm p)
+//
+// The sums leave through LDS, 32 tokens at a time (a store to LDS takes them from the accumulators' half of the register file
+// as they are), to lanes that keep the same channels for all tokens: those channels' scales stay in registers, and a lane
+// stores 16 bytes.  Its code is a loop: unrolled over the accumulators it was 72 KB that every launch fetched anew: 17 us of
+// 4096 x 4096 outputs where this takes 14.
+template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void gemm_scaled_tile_kernel(ScaledGemm p)
 {
     constexpr int EDGE = 64 * F, CHUNK = 128, SIDE = EDGE * CHUNK, STEPS = CHUNK / 32, LOADS = 2 * F;   // loads of a wave, chunk and operand
-    extern __shared__ __attribute__((aligned(16))) char gemm_lds[];      // [2 buffers][W, X][EDGE][CHUNK]
+    extern __shared__ __attribute__((aligned(16))) char gemm_lds[];      // [STAGES][W, X][EDGE][CHUNK]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, half = lane >> 5;
     const int wn = wave & 1, wm = wave >> 1;
     int tm, tn;
     tile_of(p, blockIdx.x, tm, tn);
     const int m0 = tm * EDGE, n0 = tn * EDGE;
 
-    // loader: a wave's load u covers rows 16 F wave + 8 u .. + 7 of the tile, lane l row l / 8, piece (l % 8) ^ (l / 8)
+    // loader: a wave's load u covers rows 16 F wave + 8 u .. + 7 of a side, lane l row l / 8, piece (l % 8) ^ (l / 8)
     const v4u_t from[2] = {make_raw_desc(p.W + static_cast<int64_t>(n0) * p.pitch, static_cast<uint32_t>(min(EDGE, p.N - n0)) * p.pitch),
                            make_raw_desc(p.X + static_cast<int64_t>(m0) * p.pitch, static_cast<uint32_t>(min(EDGE, p.M - m0)) * p.pitch)};
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)gemm_lds));
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     const uint32_t row_at = static_cast<uint32_t>(wave * 16 * F + (lane >> 3)) * p.pitch + piece;
     const int chunks = (p.pitch + CHUNK - 1) / CHUNK;
-    const auto load = [&](int chunk, int buf, auto uc) {
+    const auto load = [&](int chunk, int stage, auto uc) {
         constexpr int u = decltype(uc)::value, side = u / LOADS, v = u % LOADS;
         // (beyond the row's end, or the last chunk: out of the descriptor's range, so zeros)
         const uint32_t at = chunk * CHUNK + piece < p.pitch ? row_at + chunk * CHUNK : 0x80000000u;
-        load_to_lds_16(from[side], lds_base + (2 * buf + side) * SIDE + (wave * 16 * F + 8 * v) * CHUNK, at + static_cast<uint32_t>(8 * v) * p.pitch, 0);
+        load_to_lds_16(from[side], lds_base + (2 * stage + side) * SIDE + (wave * 16 * F + 8 * v) * CHUNK, at + static_cast<uint32_t>(8 * v) * p.pitch, 0);
     };
 
     // fragments of a step: rows 32 (F w + f) + r, piece (2 step + half) ^ (r % 8)
     const int frag_at = r * CHUNK + ((half ^ (r & 7)) << 4);
     i32x4_t fw[2][F], fx[2][F];
-    const auto read = [&](int buf, auto sc, auto fc) {
+    const auto read = [&](int stage, auto sc, auto fc) {
         constexpr int s = decltype(sc)::value, f = decltype(fc)::value;
-        const int at = 2 * buf * SIDE + (frag_at ^ (32 * s)) + (f % F) * 32 * CHUNK;
+        const int at = 2 * stage * SIDE + (frag_at ^ (32 * s)) + (f % F) * 32 * CHUNK;
         if constexpr (f < F) fw[s & 1][f] = *reinterpret_cast<const i32x4_t *>(gemm_lds + at + wn * 32 * F * CHUNK);
         else fx[s & 1][f - F] = *reinterpret_cast<const i32x4_t *>(gemm_lds + at + SIDE + wm * 32 * F * CHUNK);
     };
@@ -88,146 +91,166 @@ template <class T, int F> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void
     i32x16_t acc[F][F] = {};
     using I0 = std::integral_constant<int, 0>;
     constexpr int VMCNT0 = 0x0F70;
-    static_for<2 * LOADS>([&](auto u) { load(0, 0, u); });
-    static_for<2 * LOADS>([&](auto u) { load(1, 1, u); });
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");       // the first chunk has landed
+    static_for<STAGES>([&](auto st) { static_for<2 * LOADS>([&](auto u) { load(decltype(st)::value, decltype(st)::value, u); }); });
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * 2 * LOADS) : "memory");        // the first chunk has landed
     __syncthreads();
     if (chunks) static_for<2 * F>([&](auto f) { read(0, I0{}, f); });
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        const int buf = chunk & 1;
+    for (int chunk = 0, stage = 0; chunk < chunks; ++chunk) {
+        const int after = stage + 1 == STAGES ? 0 : stage + 1;
         static_for<STEPS>([&](auto sc) {
             constexpr int s = decltype(sc)::value, next = (s + 1) % STEPS;
             if constexpr (s == STEPS - 1) {
-                __builtin_amdgcn_s_waitcnt(VMCNT0);       // the next chunk has landed, and everyone has read this one
-                __syncthreads();
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * LOADS) : "memory");
+                __syncthreads();                          // the next chunk has landed, and everyone has read this one
             }
             static_for<F * F>([&](auto qc) {
                 constexpr int q = decltype(qc)::value;
                 acc[q / F][q % F] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[s & 1][q / F], fx[s & 1][q % F], acc[q / F][q % F], 0, 0, 0);
                 constexpr int reads = 2 * F * (q + 1) / (F * F) - 2 * F * q / (F * F);
                 static_for<reads>([&](auto i) {
-                    read(s == STEPS - 1 ? buf ^ 1 : buf, std::integral_constant<int, next>{}, std::integral_constant<int, 2 * F * q / (F * F) + decltype(i)::value>{});
+                    read(s == STEPS - 1 ? after : stage, std::integral_constant<int, next>{}, std::integral_constant<int, 2 * F * q / (F * F) + decltype(i)::value>{});
                 });
                 if constexpr (s == STEPS - 1) {
                     constexpr int loads = 2 * LOADS * (q + 1) / (F * F) - 2 * LOADS * q / (F * F);
-                    static_for<loads>([&](auto i) { load(chunk + 2, buf, std::integral_constant<int, 2 * LOADS * q / (F * F) + decltype(i)::value>{}); });
+                    static_for<loads>([&](auto i) { load(chunk + STAGES, stage, std::integral_constant<int, 2 * LOADS * q / (F * F) + decltype(i)::value>{}); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
+        stage = after;
     }
     __builtin_amdgcn_s_waitcnt(VMCNT0);                   // the loads beyond the last chunk are done with LDS
     __syncthreads();
 
-    // results: 32 tokens at a time through LDS, so that whole runs of channels of a token leave together
-    constexpr int ROW = 32 * F * static_cast<int>(sizeof(T)) + 16, REGION = 32 * (32 * F * 4 + 16);
-    float *const wide_scale = reinterpret_cast<float *>(gemm_lds + 4 * REGION);      // [EDGE] mantissa, exponent, bias
-    for (int i = threadIdx.x; i < EDGE; i += 256) {
-        const int n = n0 + i;
-        const Scale w = scale_of(n < p.N ? p.w_scale[n] : 0.0f);
-        wide_scale[3 * i] = w.part;
-        wide_scale[3 * i + 1] = __int_as_float(w.exponent);
-        wide_scale[3 * i + 2] = p.bias && n < p.N ? p.bias[n] : 0.0f;
-    }
-    __syncthreads();
+    constexpr int V = 16 / static_cast<int>(sizeof(T)), LANES = 32 * F / V, ROW = 32 * F * 4 + 16, REGION = 32 * ROW + 32 * F * 4;
     char *const mine = gemm_lds + wave * REGION;
+    float *const x_scale = reinterpret_cast<float *>(mine + 32 * ROW);   // of the wave's 32 F tokens
+    const int mw = m0 + wm * 32 * F, n = n0 + wn * 32 * F + lane % LANES * V;
+    float w[V], bias[V];
+    bool far = false;                                     // a scale outside 2^-60 .. 2^60: the others can be multiplied as they are
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        w[j] = n + j < p.N ? p.w_scale[n + j] : 0.0f;
+        bias[j] = p.bias && n + j < p.N ? p.bias[n + j] : 0.0f;
+        far |= abs(scale_of(w[j]).exponent) > 60;
+    }
+#pragma unroll 1
+    for (int i = lane; i < 32 * F; i += 64) {
+        const float x = mw + i < p.M ? p.x_scale[mw + i] : 0.0f;
+        x_scale[i] = x;
+        far |= abs(scale_of(x).exponent) > 60;
+    }
+    far = __any(far);
     static_for<F>([&](auto fm) {
         constexpr int b = decltype(fm)::value;
-        const int mt = m0 + (wm * F + b) * 32;
-        const Scale x = scale_of(mt + r < p.M ? p.x_scale[mt + r] : 0.0f);
         static_for<4 * F>([&](auto gc) {
             constexpr int g = decltype(gc)::value, f = g / 4;
-            const int ch = f * 32 + 8 * (g % 4) + 4 * half;           // of the wave's channels
-            T y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float *w = wide_scale + 3 * (wn * 32 * F + ch + j);
-                y[j] = static_cast<T>(scaled(acc[f][b][4 * (g % 4) + j], x, Scale{w[0], __float_as_int(w[1])}, w[2]));
-            }
-            __builtin_memcpy(mine + r * ROW + ch * sizeof(T), y, sizeof y);
+            *reinterpret_cast<i32x4_t *>(mine + r * ROW + (f * 32 + 8 * (g % 4) + 4 * half) * 4) =
+                i32x4_t{acc[f][b][4 * (g % 4)], acc[f][b][4 * (g % 4) + 1], acc[f][b][4 * (g % 4) + 2], acc[f][b][4 * (g % 4) + 3]};
         });
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        constexpr int V = 16 / static_cast<int>(sizeof(T)), LANES = 32 * F / V;       // lanes of a row
+        lds_in_order();
+        const char *from_lds = mine + lane / LANES * ROW + lane % LANES * V * 4;
+        const float *x = x_scale + 32 * b + lane / LANES;
+        int m = mw + 32 * b + lane / LANES;
+        T *to = static_cast<T *>(p.Y) + m * p.ldy + n;
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 128 / LANES) {       // two rows a lane in a turn
+            i32x4_t sum[2][V / 4];
 #pragma unroll
-        for (int i = 0; i < 32 * LANES / 64; ++i) {
-            const int at = i * 64 + lane, row = at / LANES, ch = at % LANES * V, m = mt + row, n = n0 + wn * 32 * F + ch;
-            if (m >= p.M || n >= p.N) continue;
-            const Pack16<T> v = *reinterpret_cast<const Pack16<T> *>(mine + row * ROW + ch * sizeof(T));
-            T *y = static_cast<T *>(p.Y) + m * p.ldy + n;
-            if (p.wide && n + V <= p.N) *reinterpret_cast<Pack16<T> *>(y) = v;
-            else
-                for (int j = 0; j < V && n + j < p.N; ++j) y[j] = v.v[j];
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < V / 4; ++j) sum[u][j] = *reinterpret_cast<const i32x4_t *>(from_lds + (i + u * (64 / LANES)) * ROW + 16 * j);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float xs = x[i + u * (64 / LANES)];
+                T y[V];
+                if (far)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[j] = static_cast<T>(scaled(sum[u][j / 4][j % 4], scale_of(xs), scale_of(w[j]), bias[j]));
+                else
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[j] = static_cast<T>(static_cast<float>(sum[u][j / 4][j % 4]) * xs * w[j] + bias[j]);
+                if (m < p.M && n + V <= p.N) __builtin_memcpy(to, y, sizeof y);      // (wherever a row begins)
+                else if (m < p.M)
+#pragma unroll
+                    for (int j = 0; j < V - 1; ++j)
+                        if (n + j < p.N) to[j] = y[j];
+                m += 64 / LANES;
+                to += 64 / LANES * p.ldy;
+            }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
     });
 }
 
-// Few tokens: 16 MT tokens x 16 NT channels a block, the block's waves sharing K in turns of 256 bytes.
+// Few tokens: 16 MT tokens x 16 NT channels a block, the block's waves sharing K in turns of 128 bytes.
 //
-// Bound by reading W once.  Lanes load fragments straight from memory, a load of 16 rows taking 64 neighbouring bytes of each
-// and the four loads of a turn 256 (the order of K within a turn is free, the same for both operands).  The next turn is in
-// flight while one is multiplied.  X comes from L2 again for each block: MT / NT bytes for each byte of W.
-template <class T, int MT, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES) void gemm_scaled_few_kernel(ScaledGemm p)
+// Bound by reading W once.  Lanes of a fragment read straight from memory lie a row apart, which costs the address unit four
+// times as long as neighbours do (M = 40, N = 10240, K = 5120: 35 us), so a wave brings its turns through LDS: eight
+// neighbours load a whole 128-byte line of a row, its pieces swizzled by row for the fragment reads.  A wave has LDS of its own, STAGES turns
+// of it in flight, and waits for nobody before the sums are joined.  X comes from L2 for each block: MT / NT bytes for each
+// byte of W; rows beyond M are out of the buffer's range and cost nothing.
+template <class T, int MT, int NT, int WAVES, int STAGES> __global__ __launch_bounds__(64 * WAVES) void gemm_scaled_few_kernel(ScaledGemm p)
 {
-    constexpr int TURN = 256;
-    __shared__ i32x4_t sums[WAVES][NT][MT][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
+    constexpr int TURN = 128, STAGE = (NT + MT) * 16 * TURN;
+    static_assert(STAGES * STAGE >= NT * MT * 1024, "the sums are joined in the same LDS");
+    __shared__ alignas(16) char lds[WAVES][STAGES * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, quarter = lane >> 4;
     const int n0 = static_cast<int>(blockIdx.x) % p.across * 16 * NT, m0 = static_cast<int>(blockIdx.x) / p.across * 16 * MT;
-    const int8_t *w[NT], *x[MT];
+    const v4u_t W = make_raw_desc(p.W + static_cast<int64_t>(n0) * p.pitch, static_cast<uint32_t>(min(16 * NT, p.N - n0)) * p.pitch);
+    const v4u_t X = make_raw_desc(p.X + static_cast<int64_t>(m0) * p.pitch, static_cast<uint32_t>(min(16 * MT, p.M - m0)) * p.pitch);
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)lds[wave]));
+    // loader: lane l has row l / 8 of 8, piece (l % 8) ^ (l / 8); reader: lane l row l % 16, piece 4 step + l / 16
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t row_at = static_cast<uint32_t>(lane >> 3) * p.pitch + piece;
+    const int frag_at = r * TURN + ((quarter ^ (r & 7)) << 4);
+    const auto fetch = [&](int k, int stage) {
+        const uint32_t at = k + piece < p.pitch ? row_at + k : 0x80000000u;       // beyond the row's end: out of range, so zeros
 #pragma unroll
-    for (int i = 0; i < NT; ++i) w[i] = p.W + static_cast<int64_t>(min(n0 + 16 * i + r, p.N - 1)) * p.pitch + 16 * quarter;
+        for (int i = 0; i < 2 * NT; ++i) load_to_lds_16(W, base + stage * STAGE + i * 8 * TURN, at + static_cast<uint32_t>(8 * i) * p.pitch, 0);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) x[i] = p.X + static_cast<int64_t>(min(m0 + 16 * i + r, p.M - 1)) * p.pitch + 16 * quarter;
-    i32x4_t acc[NT][MT] = {};
-    struct Turn { i32x4_t a[4][NT], b[4][MT]; };
-    const auto fetch = [&](int k) {
-        Turn t;
-        const bool whole = k + TURN <= p.pitch;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool in = whole || k + 16 * quarter + 64 * j < p.pitch;
-            const int at = in ? k + 64 * j : -16 * quarter;            // (beyond the end: the row's first bytes, for nothing)
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                t.a[j][i] = *reinterpret_cast<const i32x4_t *>(w[i] + at);
-                if (!in) t.a[j][i] = i32x4_t{};
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) t.b[j][i] = *reinterpret_cast<const i32x4_t *>(x[i] + at);
-        }
-        return t;
+        for (int i = 0; i < 2 * MT; ++i) load_to_lds_16(X, base + stage * STAGE + (2 * NT + i) * 8 * TURN, at + static_cast<uint32_t>(8 * i) * p.pitch, 0);
     };
-    const auto multiply = [&](const Turn &t) {
+    i32x4_t acc[NT][MT] = {};
+    int k = wave * TURN, stage = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+    for (int s = 0; s < STAGES; ++s) fetch(k + s * WAVES * TURN, s);
+    for (; k < p.pitch; k += WAVES * TURN) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * 2 * (NT + MT)) : "memory"); // the oldest turn has landed
+        i32x4_t w[2][NT], x[2][MT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const char *from = lds[wave] + stage * STAGE + (frag_at ^ (64 * s));
+#pragma unroll
+            for (int i = 0; i < NT; ++i) w[s][i] = *reinterpret_cast<const i32x4_t *>(from + i * 16 * TURN);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x[s][i] = *reinterpret_cast<const i32x4_t *>(from + (NT + i) * 16 * TURN);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                  // and is in registers before its place is taken
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(k + STAGES * WAVES * TURN, stage);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int l = 0; l < MT; ++l) acc[i][l] = __builtin_amdgcn_mfma_i32_16x16x64_i8(t.a[j][i], t.b[j][l], acc[i][l], 0, 0, 0);
-    };
-    int k = wave * TURN;
-    if (k < p.pitch) {
-        Turn now = fetch(k);
-        for (k += WAVES * TURN; k < p.pitch; k += WAVES * TURN) {
-            const Turn next = fetch(k);
-            multiply(now);
-            now = next;
-        }
-        multiply(now);
+                for (int l = 0; l < MT; ++l) acc[i][l] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s][i], x[s][l], acc[i][l], 0, 0, 0);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                      // nothing is on its way to LDS any more
+    i32x4_t *const sums = reinterpret_cast<i32x4_t *>(lds);              // [WAVES][NT][MT][64]
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int l = 0; l < MT; ++l) sums[wave][i][l][lane] = acc[i][l];
+        for (int l = 0; l < MT; ++l) sums[((wave * NT + i) * MT + l) * 64 + lane] = acc[i][l];
     __syncthreads();
     for (int t = threadIdx.x; t < NT * MT * 64; t += 64 * WAVES) {
         const int at = t & 63, l = t / 64 % MT, i = t / 64 / MT, m = m0 + 16 * l + (at & 15), n = n0 + 16 * i + 4 * (at >> 4);
         if (m >= p.M) continue;
-        i32x4_t sum = sums[0][i][l][at];
+        i32x4_t sum = sums[t];
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += sums[v][i][l][at];
+        for (int v = 1; v < WAVES; ++v) sum += sums[v * NT * MT * 64 + t];
         const Scale sx = scale_of(p.x_scale[m]);
         T *y = static_cast<T *>(p.Y) + m * p.ldy + n;
 #pragma unroll
@@ -236,37 +259,56 @@ template <class T, int MT, int NT, int WAVES> __global__ __launch_bounds__(64 * 
     }
 }
 
-template <class T, int F> int launch_tiles(ScaledGemm p, hipStream_t st)
+template <class T, int F, int STAGES> int launch_tiles(ScaledGemm p, hipStream_t st)
 {
-    constexpr int edge = 64 * F, bytes = 4 * edge * 128;
+    constexpr int edge = 64 * F, bytes = STAGES * 2 * edge * 128;
     p.across = static_cast<int>(ceil_div(p.N, edge));
     p.tiles = p.across * static_cast<int>(ceil_div(p.M, edge));
     if constexpr (bytes > 64 * 1024) {
         static std::atomic<uint64_t> granted{0};
-        if (!all_of_lds(gemm_scaled_tile_kernel<T, F>, granted)) return fail(APNN_ERR_DEVICE, "apnn_gemm_scaled: no %d bytes of LDS", bytes);
+        if (!all_of_lds(gemm_scaled_tile_kernel<T, F, STAGES>, granted)) return fail(APNN_ERR_DEVICE, "apnn_gemm_scaled: no %d bytes of LDS", bytes);
     }
-    gemm_scaled_tile_kernel<T, F><<<static_cast<unsigned>(p.tiles), 256, bytes, st>>>(p);
+    gemm_scaled_tile_kernel<T, F, STAGES><<<static_cast<unsigned>(p.tiles), 256, bytes, st>>>(p);
     return check_launch("apnn_gemm_scaled");
 }
 
-template <class T, int MT, int NT> int launch_few(ScaledGemm p, hipStream_t st)
+template <class T, int MT, int NT, int WAVES, int STAGES> int launch_few(ScaledGemm p, hipStream_t st)
 {
     p.across = static_cast<int>(ceil_div(p.N, 16 * NT));
     p.tiles = p.across * static_cast<int>(ceil_div(p.M, 16 * MT));
-    gemm_scaled_few_kernel<T, MT, NT, 8><<<static_cast<unsigned>(p.tiles), 512, 0, st>>>(p);
+    gemm_scaled_few_kernel<T, MT, NT, WAVES, STAGES><<<static_cast<unsigned>(p.tiles), 64 * WAVES, 0, st>>>(p);
     return check_launch("apnn_gemm_scaled");
 }
 
 template <class T> int launch_scaled(const ScaledGemm &p, hipStream_t st)
 {
-    if (p.M <= 16) return launch_few<T, 1, 1>(p, st);
-    if (p.M <= 32) return launch_few<T, 2, 2>(p, st);
-    if (p.M <= 48) return launch_few<T, 3, 2>(p, st);
-    if (p.M <= 64) return launch_few<T, 4, 2>(p, st);
+    // Few tokens: the more channels a block has, the less often X is read, as long as most compute units get a block
+    // (M = 40, N = 10240, K = 5120: 22.2, 21.2, 17.6, 19.3 us with 1 .. 4 tiles of channels; M = 64, N = K = 4096: 8.7, 9.8, -, 12.7).
+    const int64_t units = ceil_div(p.N, 16);
+    const auto few = [&](auto tokens, int wide) {
+        constexpr int MT = decltype(tokens)::value;
+        if (wide >= 4) return launch_few<T, MT, 4, 4, 1>(p, st);
+        if (wide == 3) return launch_few<T, MT, 3, 4, 1>(p, st);
+        if (wide == 2) return launch_few<T, MT, 2, 4, 1>(p, st);
+        return launch_few<T, MT, 1, 4, MT == 4 ? 1 : 2>(p, st);
+    };
+    const int wide = static_cast<int>(units / 192);
+    if (p.M <= 16) return launch_few<T, 1, 1, 4, 2>(p, st);
+    if (p.M <= 32) return few(std::integral_constant<int, 2>{}, wide);
+    if (p.M <= 48) return few(std::integral_constant<int, 3>{}, wide);
+    if (p.M <= 64) return few(std::integral_constant<int, 4>{}, wide);
+    // A few more: 64 tokens a block while that is about one block a compute unit and reads nothing often
+    // (M = 256, N = 1000, K = 1999: 7.6 us, 64 x 64 tiles 9.6; M = 128, N = K = 4096: 10.3, 11.6; M = 200: 13.6, 12.1).
+    const int64_t down = ceil_div(p.M, 64);
+    const int64_t least = ceil_div(units * down, 320);
+    if (least <= 4 && (down <= 2 || least == 1)) return few(std::integral_constant<int, 4>{}, static_cast<int>(least));
+    // Tiles: rounds of blocks by what a round takes (us at K = 4096: 64-wide tiles 9 and 3 once, 128-wide 22 a block to a compute
+    // unit and 38 two, 256-wide 67).
     const auto blocks = [&](int edge) { return ceil_div(p.M, edge) * ceil_div(p.N, edge); };
-    if (blocks(256) >= 192) return launch_tiles<T, 4>(p, st);
-    if (blocks(128) >= 192) return launch_tiles<T, 2>(p, st);
-    return launch_tiles<T, 1>(p, st);
+    const int64_t small = 3 + 9 * ceil_div(blocks(64), 256), middle = blocks(128) <= 256 ? 22 : 38 * ceil_div(blocks(128), 512), large = 67 * ceil_div(blocks(256), 256);
+    if (large <= small && large <= middle) return launch_tiles<T, 4, 2>(p, st);
+    if (small < middle) return launch_tiles<T, 1, 4>(p, st);
+    return blocks(128) <= 256 ? launch_tiles<T, 2, 4>(p, st) : launch_tiles<T, 2, 2>(p, st);
 }
 
 }  // namespace apnn
@@ -286,7 +328,6 @@ extern "C" int apnn_gemm_scaled(const int8_t *X_dev, const float *x_scale_dev, c
     if (!aligned_to(Y_dev, type)) return fail(APNN_ERR_ALIGNMENT, "apnn_gemm_scaled: Y is not aligned to its type");
     if (M > (1 << 26) || N > (1 << 26) || M * N > (int64_t(1) << 35) || ldy > INT64_MAX / 8 / M)
         return fail(APNN_ERR_UNSUPPORTED, "apnn_gemm_scaled: M = %lld, N = %lld, ldy = %lld", (long long)M, (long long)N, (long long)ldy);
-    ScaledGemm p = {X_dev, W_dev, x_scale_dev, w_scale_dev, bias_dev, Y_dev, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(apnn_token_pitch(K)), 0, 0, false};
-    p.wide = aligned16(Y_dev) && ldy * size_of(type) % 16 == 0;
+    const ScaledGemm p = {X_dev, W_dev, x_scale_dev, w_scale_dev, bias_dev, Y_dev, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(apnn_token_pitch(K)), 0, 0};
     return by_type(type, [&](auto t) { return launch_scaled<decltype(t)>(p, as_stream(stream)); });
 }

@@ -6,6 +6,7 @@
 // (ds_read_b64_tr_b16).  A 4-bit group with its power of two is exact in 16 bits, so the conversion
 // (v_cvt_scalef32_pk_*_fp4, two values an instruction) costs no accuracy: keys take the queries' type, values fp16.
 #include "kv_cache.h"
+#include "lds_load.h"
 
 namespace apnn {
 
@@ -258,8 +259,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                 p[4 * u + j] = static_cast<_Float16>(e);
             }
         sum = sum * keep + part;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // this wave's values are in LDS (its accesses stay in order)
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
             const char *from = mine + (4 * quarter + (c >> 2)) * kValueRow<D> + (16 * d + 4 * (c & 3)) * 2;
@@ -272,8 +272,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
             }
             out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, out[d] * keep, 0, 0, 0);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
         now = next;
     }
     sum += __shfl_xor(sum, 16);

@@ -34,4 +34,11 @@ __device__ __forceinline__ void load_to_lds_16(v4u_t desc, uint32_t lds_base, ui
                  : "memory", "m0");
 }
 
+// Between LDS accesses of one wave to memory of its own: the hardware keeps them in order, the compiler has to as well.
+__device__ __forceinline__ void lds_in_order()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 }  // namespace apnn
