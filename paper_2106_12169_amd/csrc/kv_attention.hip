@@ -11,16 +11,18 @@
 namespace apnn {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 struct AttentionArgs {
     apnn_kv_attention_desc d;
     apnn_kv_cache c;
     float *parts;                                         // workspace
-    int64_t tiles;                                        // 16-row tiles of max_q * group rows
+    int64_t tiles;                                        // tiles of max_q * group rows
     int page_shift, group;                                // query heads to a cache head
     int splits, part_rows;                                // of a tile's tokens; rows of a tile that there can be
-    bool q_aligned;                                       // queries can be read 16 bytes at a time
+    int tile_rows;                                        // 16 or 128
 };
 
 // 16-bit operand types of the scores
@@ -33,6 +35,7 @@ template <> struct Operand<_Float16> {
     static __device__ __forceinline__ uint32_t two(uint32_t w, float unit, std::integral_constant<int, 3>) { return bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, unit, 3)); }
     static __device__ __forceinline__ uint32_t bits(half2_t v) { return __builtin_bit_cast(uint32_t, v); }
     static __device__ __forceinline__ f32x4_t product(vec a, vec b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16_t product(vec a, vec b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 template <> struct Operand<__bf16> {
     typedef bf16x8_t vec;
@@ -42,6 +45,7 @@ template <> struct Operand<__bf16> {
     static __device__ __forceinline__ uint32_t two(uint32_t w, float unit, std::integral_constant<int, 3>) { return bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, 3)); }
     static __device__ __forceinline__ uint32_t bits(bf16x2_t v) { return __builtin_bit_cast(uint32_t, v); }
     static __device__ __forceinline__ f32x4_t product(vec a, vec b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x16_t product(vec a, vec b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -78,20 +82,19 @@ template <int D> constexpr int kValueRow = 2 * D + 32;
 // Over the four lanes that share a column (lane ^ 16, lane ^ 32).
 __device__ __forceinline__ float column_max(float x)
 {
-    typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
     u32x2_t y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
     y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
-// What a block works on: 16 rows (queries x the heads that share a cache head, heads inside) of one sequence and cache head.
+// What a block works on: 16 or 128 rows (queries x the heads that share a cache head, heads inside) of one sequence and cache head.
 struct Rows {
     int64_t q0;                                           // first query row of the sequence
     int n, all, have;                                     // its queries, at most max_q of them and all; its tokens that the table can name
     int shift;                                            // query i sees have' = min(have, shift + i + 1) tokens
     int r0;                                               // first row of the tile
-    int most;                                             // tokens that any of the 16 rows sees
+    int most;                                             // tokens that any of the rows sees
     bool any;
 };
 
@@ -110,15 +113,28 @@ __device__ __forceinline__ Rows find_rows(const AttentionArgs &a, int64_t b, int
     n = n < a.d.tokens - x.q0 ? n : a.d.tokens - x.q0;
     x.all = static_cast<int>(n);
     x.n = static_cast<int>(n < a.d.max_q ? n : a.d.max_q);
-    if (tile * 16 >= int64_t(x.n) * a.group) return x;
+    if (tile * a.tile_rows >= int64_t(x.n) * a.group) return x;
     x.any = true;
-    x.r0 = static_cast<int>(tile * 16);
+    x.r0 = static_cast<int>(tile * a.tile_rows);
     const int len = a.d.len_dev[b], room = static_cast<int>(a.d.max_pages << a.page_shift);
     x.have = min(max(len, 0), room);
     x.shift = max(len, 0) - x.all;
-    const int last = min((x.r0 + 15) / a.group, x.n - 1);
+    const int last = min((x.r0 + a.tile_rows - 1) / a.group, x.n - 1);
     x.most = seen_by(x, last);
     return x;
+}
+
+// Tile, cache head and sequence of a block.  Heads and sequences change fastest: blocks go to the eight XCDs in turn, so that the
+// tiles of one head find its codes in the L2 of the same XCD as long as heads x seqs is a multiple of 8; the tiles that see the
+// most tokens come first.
+struct Place {
+    int64_t tile, seq;
+    int head;
+};
+__device__ __forceinline__ Place place_of(const AttentionArgs &a, int64_t unit)
+{
+    const int64_t pairs = a.d.seqs * a.c.heads, turn = quotient(unit, pairs), pair = unit - turn * pairs, seq = quotient(pair, a.c.heads);
+    return {a.tiles - 1 - turn, seq, static_cast<int>(pair - seq * a.c.heads)};
 }
 
 // Tokens of a split: a tile's tokens over `splits`, whole turns of the block's waves, and no fewer than pay for the joining.
@@ -149,13 +165,12 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     __shared__ float row_max[4][16], row_sum[4][16];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, quarter = lane >> 4;
-    int64_t id = first + blockIdx.x;
-    const int split = SPLIT ? static_cast<int>(id % a.splits) : 0;
-    const int64_t unit = SPLIT ? id / a.splits : id, tile = unit % a.tiles, rest = unit / a.tiles;
-    const int head = static_cast<int>(rest % a.c.heads);
-    const int64_t b = rest / a.c.heads;
-    if (b >= a.d.seqs) return;
-    const Rows x = find_rows(a, b, tile);
+    const int64_t id = first + blockIdx.x, unit = SPLIT ? quotient(id, a.splits) : id;
+    const int split = SPLIT ? static_cast<int>(id - unit * a.splits) : 0;
+    const Place place = place_of(a, unit);
+    const int64_t b = place.seq;
+    const int head = place.head;
+    const Rows x = find_rows(a, b, place.tile);
     if (!x.any) return;
     int begin = 0, end = x.most;
     if (SPLIT) {
@@ -172,15 +187,8 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     {
         const int qh = head * a.group + (live ? r - i * a.group : 0);
         const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + quarter * (D / 4);
-        if (a.q_aligned) {
 #pragma unroll
-            for (int s = 0; s < steps; ++s) q[s] = *reinterpret_cast<const typename Op::vec *>(src + 8 * s);
-        } else {
-#pragma unroll
-            for (int s = 0; s < steps; ++s)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[s][j] = src[8 * s + j];
-        }
+        for (int s = 0; s < steps; ++s) __builtin_memcpy(&q[s], src + 8 * s, 16);        // (however they are aligned)
     }
     const float factor = a.d.scale * 1.4426950408889634f; // scores in powers of two
     const int32_t *pages = a.d.page_dev + b * a.d.max_pages;
@@ -314,17 +322,214 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     }
 }
 
+// Two lanes that share a column of the 32 x 32 instruction (lane ^ 32).
+__device__ __forceinline__ u32x2_t both_halves(float x) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false); }
+
+// Bytes between rows of keys and values in LDS of the kernel for many rows: fragment reads of 8 key rows, and transposing reads
+// of 64 bytes of 4 value rows, cover all banks.
+template <int D> constexpr int kManyKeyRow = 2 * D + 16;
+template <int D> constexpr int kManyValueRow = D == 96 ? 320 : 2 * D + 64;
+template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<D>);
+
+// 128 query rows of one cache head against one split of the sequence, 32 rows a wave, 64 tokens at a time.
+//
+// Bound by the matrix unit and the vector instructions of the softmax, which two blocks on a compute unit overlap (one where
+// D = 256).  The tokens' codes are converted once for all rows, into two tiles of LDS in turn: while one is multiplied, the next
+// is converted and the codes of the one after are on their way.  As for 16 rows, scores are computed transposed and the weights
+// stay in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
+// values are read in that order.  The maximum that weights refer to moves only when a score exceeds it by 2^8, which fp16
+// weights and fp32 sums have room for, so that accumulators are rarely rescaled.
+template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
+{
+    using Op = Operand<T>;
+    constexpr int steps = D / 16, tokens = 64, words = Share<D>::words;
+    extern __shared__ __attribute__((aligned(16))) char many_lds[];      // [2][keys, values], then [2][4] pages that are there
+    uint8_t *const pages_there = reinterpret_cast<uint8_t *>(many_lds + 2 * kManyTile<D>);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
+    const int64_t id = first + blockIdx.x, unit = SPLIT ? quotient(id, a.splits) : id;
+    const int split = SPLIT ? static_cast<int>(id - unit * a.splits) : 0;
+    const Place place = place_of(a, unit);
+    const int head = place.head;
+    const Rows x = find_rows(a, place.seq, place.tile);
+    if (!x.any) return;
+    int begin = 0, end = x.most;
+    if (SPLIT) {
+        const int each = split_tokens(x.most, a.splits);
+        if (split && static_cast<int64_t>(split) * each >= x.most) return;
+        begin = split * each;
+        end = min(begin + each, x.most);
+    }
+
+    const int r = x.r0 + 32 * wave + c, i = r / a.group;
+    const bool live = i < x.n;
+    const int seen = live ? seen_by(x, i) : 0;
+    // every row of the wave sees the tokens before `least`, none one from `mine` on
+    const int wave_first = x.r0 + 32 * wave, rows = x.n * a.group;
+    const int least = wave_first + 31 < rows ? seen_by(x, wave_first / a.group) : 0;
+    const int mine = wave_first < rows ? seen_by(x, min((wave_first + 31) / a.group, x.n - 1)) : 0;
+    typename Op::vec q[steps];
+    {
+        const int qh = head * a.group + (live ? r - i * a.group : 0);
+        const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + 8 * half;
+        const uint32_t flip = a.d.scale < 0.0f ? 0x80008000u : 0u;       // a negative scale is the queries'
+#pragma unroll
+        for (int s = 0; s < steps; ++s) {
+            u32x4_t w;
+            __builtin_memcpy(&w, src + 16 * s, 16);
+            q[s] = __builtin_bit_cast(typename Op::vec, w ^ flip);
+        }
+    }
+    const float factor = fabsf(a.d.scale) * 1.4426950408889634f;         // scores in powers of two
+    const int32_t *pages = a.d.page_dev + place.seq * a.d.max_pages;
+    const int mask = (1 << a.page_shift) - 1;
+
+    // loader: thread 4 t + u has token t of a tile and channels [D / 4 u, + D / 4)
+    const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+    struct Row { Codes<D> k, v; uint8_t ku[Share<D>::units], vu[Share<D>::units]; bool there, written; };
+    const auto fetch = [&](int t0) {
+        Row f;
+        const int t = t0 + token, page = pages[t < end ? t >> a.page_shift : 0];         // (tokens there are, so there is a first page)
+        f.there = t < end && page >= 0 && page < a.c.pages;
+        f.written = f.there && t < x.have;
+        const int64_t row = ((static_cast<int64_t>(f.there ? page : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
+        const int64_t code_at = row * (D / 2) + quarter * (D / 8), unit_at = row * (D / 32) + quarter * (D / 4) / 32;
+        f.k = *reinterpret_cast<const Codes<D> *>(a.c.k_codes_dev + code_at);
+        f.v = *reinterpret_cast<const Codes<D> *>(a.c.v_codes_dev + code_at);
+#pragma unroll
+        for (int y = 0; y < Share<D>::units; ++y) {
+            const int64_t at = unit_at + (y ? Share<D>::unit(quarter, words - 1) : 0);
+            f.ku[y] = a.c.k_scale_dev[at];
+            f.vu[y] = a.c.v_scale_dev[at];
+        }
+        return f;
+    };
+    const auto convert = [&](const Row &f, int buf) {
+        char *const k_to = many_lds + buf * kManyTile<D> + token * kManyKeyRow<D> + quarter * (D / 2);
+        char *const v_to = many_lds + buf * kManyTile<D> + 64 * kManyKeyRow<D> + token * kManyValueRow<D> + quarter * (D / 2);
+#pragma unroll
+        for (int s = 0; s < words; ++s) {
+            const bool second = Share<D>::units > 1 && Share<D>::unit(quarter, s);
+            *reinterpret_cast<u32x4_t *>(k_to + 16 * s) = values8<T>(f.k.w[s], unit_of(f.ku[second ? Share<D>::units - 1 : 0]));
+            *reinterpret_cast<u32x4_t *>(v_to + 16 * s) = values8<_Float16>(f.v.w[s], unit_of(f.written ? f.vu[second ? Share<D>::units - 1 : 0] : 127));
+        }
+        if ((threadIdx.x & 63) == 0) pages_there[4 * buf + token / 16] = f.there;
+    };
+
+    f32x16_t out[D / 32] = {};
+    float top = -INFINITY, sum = 0.0f;                    // what the column's weights refer to; this lane's part of their sum
+    Row next = {};
+    if (begin < end) {
+        convert(fetch(begin), 0);
+        next = fetch(begin + tokens);
+    }
+    __syncthreads();
+    for (int t0 = begin, buf = 0; t0 < end; t0 += tokens, buf ^= 1) {
+        const Row later = fetch(t0 + 2 * tokens);
+        convert(next, buf ^ 1);                           // (after the last tile: of nothing that is read)
+        next = later;
+        if (t0 < mine) {
+            const char *const keys = many_lds + buf * kManyTile<D>, *const values = keys + 64 * kManyKeyRow<D>;
+            f32x16_t score[2] = {};
+#pragma unroll
+            for (int s = 0; s < steps; ++s)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const u32x4_t k = *reinterpret_cast<const u32x4_t *>(keys + (32 * u + c) * kManyKeyRow<D> + 32 * s + 16 * half);
+                    score[u] = Op::product(__builtin_bit_cast(typename Op::vec, k), q[s], score[u]);
+                }
+            const uint32_t there = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t *>(pages_there + 4 * buf));
+            if (t0 + tokens > least || there != 0x01010101u) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const bool page = there >> (16 * u + 8 * (j / 8)) & 1;
+                        if (!(page && t0 + 32 * u + 8 * (j / 4) + 4 * half + j % 4 < seen)) score[u][j] = -INFINITY;
+                    }
+            }
+            float best = score[0][0];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) best = fmaxf(best, score[u][j]);
+            const u32x2_t two = both_halves(best);
+            best = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * factor;
+            if (__any(best > top + 8.0f)) {
+                const float higher = fmaxf(top, best), base = higher == -INFINITY ? 0.0f : higher, keep = __builtin_amdgcn_exp2f(top - base);
+                top = higher;
+                sum *= keep;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) out[d][j] *= keep;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+            half8_t p[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(score[u][j], factor, -base));
+                    sum += e;
+                    p[2 * u + j / 8][j % 8] = static_cast<_Float16>(e);
+                }
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d) {
+                    const char *from = values + (16 * s + 4 * half + (lane % 16 >> 2)) * kManyValueRow<D> + (32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4)) * 2;
+                    half8_t v;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(from + 8 * h * kManyValueRow<D>));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[4 * h + j] = __builtin_bit_cast(_Float16, static_cast<short>(y[j]));
+                    }
+                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[s], out[d], 0, 0, 0);
+                }
+        }
+        __syncthreads();
+    }
+    const u32x2_t two = both_halves(sum);
+    sum = __uint_as_float(two[0]) + __uint_as_float(two[1]);
+    if (!live) return;
+    if (SPLIT) {
+        float *part = part_of<D>(a, unit, split, 32 * wave + c);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<f32x4_t *>(part + 32 * d + 8 * j + 4 * half) = f32x4_t{out[d][4 * j], out[d][4 * j + 1], out[d][4 * j + 2], out[d][4 * j + 3]};
+        if (half == 0) {
+            part[D] = top;
+            part[D + 1] = sum;
+        }
+        return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + i) * a.d.out_token_stride + (head * a.group + (r - i * a.group)) * a.d.out_head_stride + 4 * half;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            T y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(out[d][4 * j + e] * inv);
+            __builtin_memcpy(to + 32 * d + 8 * j, y, sizeof y);
+        }
+}
+
 // Joins the splits' parts of one row, a block a row: D / 4 lanes take its channels, the others further splits.
 template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a, int64_t first)
 {
     constexpr int lanes = D / 4, teams = 256 / lanes;
     __shared__ f32x4_t sums[teams][lanes];
     __shared__ float weights[teams];
-    const int64_t id = first + blockIdx.x, unit = id / a.part_rows, tile = unit % a.tiles, rest = unit / a.tiles;
-    const int row = static_cast<int>(id - unit * a.part_rows), head = static_cast<int>(rest % a.c.heads);
-    const int64_t b = rest / a.c.heads;
-    if (b >= a.d.seqs) return;
-    const Rows x = find_rows(a, b, tile);
+    const int64_t id = first + blockIdx.x, unit = quotient(id, a.part_rows);
+    const int row = static_cast<int>(id - unit * a.part_rows);
+    const Place place = place_of(a, unit);
+    const int head = place.head;
+    const Rows x = find_rows(a, place.seq, place.tile);
     const int rr = x.r0 + row, ri = rr / a.group;
     if (!x.any || ri >= x.n) return;
     const int each = split_tokens(x.most, a.splits), parts = max(1, (x.most + each - 1) / each);
@@ -384,11 +589,11 @@ int check_attention(const char *who, const apnn_kv_attention_desc *d, const apnn
 
 namespace apnn {
 
-// How a call is cut: 16-row tiles, and splits of their tokens where tiles are too few to fill the chip.  A compute unit holds
-// four blocks; twice as many blocks as that leave room for sequences of different lengths.
+// How a call is cut: tiles of 16 or 128 rows, and splits of their tokens where tiles are too few to fill the chip.  A compute unit
+// holds four blocks of the one and two of the other; twice as many of the first leave room for sequences of different lengths.
 struct AttentionPlan {
     int64_t max_q, tiles;
-    int splits, part_rows;
+    int splits, part_rows, tile_rows;
     size_t bytes;
 };
 
@@ -398,10 +603,12 @@ static AttentionPlan plan_attention(const apnn_kv_attention_desc &d, const apnn_
     const int group = d.q_heads / c.heads;
     p.max_q = d.q_start_dev ? (d.max_q < d.tokens ? d.max_q : d.tokens) : 1;
     if (d.tokens == 0 || d.seqs == 0 || p.max_q == 0) return p;
-    p.tiles = ceil_div(p.max_q * group, 16);
-    p.part_rows = static_cast<int>(p.max_q * group < 16 ? p.max_q * group : 16);
-    const int64_t blocks = p.tiles * c.heads * d.seqs, room = d.max_pages * c.page_size;
-    int64_t splits = ceil_div(2048, blocks);
+    const int64_t rows = p.max_q * group, pairs = static_cast<int64_t>(c.heads) * d.seqs, room = d.max_pages * c.page_size;
+    p.tile_rows = rows >= 64 ? 128 : 16;
+    p.tiles = ceil_div(rows, p.tile_rows);
+    p.part_rows = static_cast<int>(rows < p.tile_rows ? rows : p.tile_rows);
+    const int64_t blocks = p.tiles * pairs;
+    int64_t splits = (p.tile_rows == 16 ? 2048 : 512) / blocks;
     if (splits > ceil_div(room, kLeastSplit)) splits = ceil_div(room, kLeastSplit);
     p.splits = splits < 1 ? 1 : static_cast<int>(splits);
     if (p.splits > 1) p.bytes = static_cast<size_t>(blocks) * p.splits * p.part_rows * (c.D + 4) * sizeof(float);
@@ -438,13 +645,14 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
     a.c = *cache;
     a.d.max_q = plan.max_q;
     if (cache->pages == 0) a.d.max_pages = 0;             // no page can be read
+    if (desc->scale == 0.0f) a.d.scale = 1e-37f;          // every weight 1 (no score reaches 2^40), and -inf, an unseen token, stays what it is
     a.parts = static_cast<float *>(workspace_dev);
     a.tiles = plan.tiles;
     a.page_shift = shift_of(cache->page_size);
     a.group = desc->q_heads / cache->heads;
     a.splits = plan.splits;
     a.part_rows = plan.part_rows;
-    a.q_aligned = aligned16(desc->q_dev) && desc->q_token_stride % 8 == 0 && desc->q_head_stride % 8 == 0;
+    a.tile_rows = plan.tile_rows;
     const int64_t units = a.tiles * cache->heads * desc->seqs;
     const auto sliced = [](int64_t blocks, auto &&launch) {
         for (int64_t first = 0; first < blocks; first += kMaxBlocks) launch(first, static_cast<unsigned>(blocks - first < kMaxBlocks ? blocks - first : kMaxBlocks));
@@ -452,12 +660,22 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
     const auto go = [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
-        if (a.splits == 1) {
+        if (a.tile_rows == 128) {
+            constexpr int bytes = 2 * kManyTile<D> + 16;
+            if constexpr (bytes > 64 * 1024) {
+                static std::atomic<uint64_t> granted[2];
+                if (!all_of_lds(kv_attention_many_kernel<T, D, false>, granted[0]) || !all_of_lds(kv_attention_many_kernel<T, D, true>, granted[1]))
+                    return fail(APNN_ERR_DEVICE, "%s: no %d bytes of LDS", who, bytes);
+            }
+            if (a.splits == 1) sliced(units, [&](int64_t first, unsigned blocks) { kv_attention_many_kernel<T, D, false><<<blocks, 256, bytes, as_stream(stream)>>>(a, first); });
+            else sliced(units * a.splits, [&](int64_t first, unsigned blocks) { kv_attention_many_kernel<T, D, true><<<blocks, 256, bytes, as_stream(stream)>>>(a, first); });
+        } else if (a.splits == 1) {
             sliced(units, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, false><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         } else {
             sliced(units * a.splits, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
-            sliced(units * a.part_rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         }
+        if (a.splits > 1)
+            sliced(units * a.part_rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         return check_launch(who);
     };
     return by_channels(cache->D, [&](auto d) { return desc->type == APNN_F16 ? go(_Float16{}, d) : go(__bf16{}, d); });
