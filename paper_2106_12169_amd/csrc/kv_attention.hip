@@ -13,6 +13,7 @@ namespace apnn {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 struct AttentionArgs {
@@ -48,8 +49,6 @@ template <> struct Operand<__bf16> {
     static __device__ __forceinline__ f32x16_t product(vec a, vec b, f32x16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
 // Eight 4-bit codes -> eight operands.
 template <class T> __device__ __forceinline__ u32x4_t values8(uint32_t w, float unit)
 {
@@ -61,13 +60,38 @@ template <class T> __device__ __forceinline__ u32x4_t values8(uint32_t w, float 
 // A row's scale as the conversions take it; 255 stands for NaN there too.
 __device__ __forceinline__ float unit_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// A lane's share of a row: lane l of a wave has token l % 16 of 16 and channels [D / 4 * (l / 16), + D / 4).
+// A quarter's share of a row: channels [D / 4 * quarter, + D / 4).  In a matrix instruction lane l has quarter l / 16 of token
+// l % 16; loaded neighbours lie side by side in the cache, lane l with quarter l % 4 of token l / 4.
 template <int D> struct Share {
     static constexpr int words = D / 32;                  // 32-bit words of codes
     static constexpr int units = D == 96 || D == 256 ? 2 : 1;             // groups of 32 channels it reaches into
     static __device__ __forceinline__ int unit(int quarter, int word) { return (quarter * (D / 4) + 8 * word) / 32 - quarter * (D / 4) / 32; }
 };
 template <int D> struct Codes { uint32_t w[Share<D>::words]; };
+
+// A share to LDS and back (word by word: a copy of the whole would keep it in memory).
+template <int D> __device__ __forceinline__ void put_codes(char *to, const Codes<D> &c)
+{
+    if constexpr (D % 128 == 0)
+#pragma unroll
+        for (int s = 0; s < Share<D>::words; s += 4) *reinterpret_cast<u32x4_t *>(to + 4 * s) = u32x4_t{c.w[s], c.w[s + 1], c.w[s + 2], c.w[s + 3]};
+    else
+#pragma unroll
+        for (int s = 0; s < Share<D>::words; ++s) *reinterpret_cast<uint32_t *>(to + 4 * s) = c.w[s];
+}
+template <int D> __device__ __forceinline__ void take_codes(const char *from, Codes<D> &c)
+{
+    if constexpr (D % 128 == 0)
+#pragma unroll
+        for (int s = 0; s < Share<D>::words; s += 4) {
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(from + 4 * s);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c.w[s + j] = w[j];
+        }
+    else
+#pragma unroll
+        for (int s = 0; s < Share<D>::words; ++s) c.w[s] = *reinterpret_cast<const uint32_t *>(from + 4 * s);
+}
 
 // Keys and values of 32 tokens as they lie in the cache.
 template <int D> struct Fetched {
@@ -137,6 +161,17 @@ __device__ __forceinline__ Place place_of(const AttentionArgs &a, int64_t unit)
     return {a.tiles - 1 - turn, seq, static_cast<int>(pair - seq * a.c.heads)};
 }
 
+// A sequence's page numbers, by scalar loads (no kernel writes a page table).
+typedef const __attribute__((address_space(4))) int32_t *PageTable;
+__device__ __forceinline__ PageTable table_of(const AttentionArgs &a, int64_t seq)
+{
+    return reinterpret_cast<PageTable>(reinterpret_cast<uintptr_t>(a.d.page_dev + seq * a.d.max_pages));
+}
+
+// The maximum that weights refer to moves only when a score exceeds it by this, in powers of two: fp16 weights and fp32 sums have
+// room for 2^8, and accumulators are rarely rescaled.
+constexpr float kSlack = 8.0f;
+
 // Tokens of a split: a tile's tokens over `splits`, whole turns of the block's waves, and no fewer than pay for the joining.
 constexpr int kTurn = 128, kLeastSplit = 256;
 __host__ __device__ __forceinline__ int split_tokens(int most, int splits)
@@ -182,92 +217,106 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
 
     const int r = x.r0 + c, i = r / a.group;
     const bool live = i < x.n;
-    const int seen = live ? seen_by(x, i) : 0;
+    const int seen = live ? seen_by(x, i) : 0, least = seen_by(x, x.r0 / a.group);       // (all rows see the tokens before `least`)
     typename Op::vec q[steps];
     {
         const int qh = head * a.group + (live ? r - i * a.group : 0);
         const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + quarter * (D / 4);
+        const uint32_t flip = a.d.scale < 0.0f ? 0x80008000u : 0u;       // a negative scale is the queries'
 #pragma unroll
-        for (int s = 0; s < steps; ++s) __builtin_memcpy(&q[s], src + 8 * s, 16);        // (however they are aligned)
+        for (int s = 0; s < steps; ++s) {
+            u32x4_t w;
+            __builtin_memcpy(&w, src + 8 * s, 16);        // (however they are aligned)
+            q[s] = __builtin_bit_cast(typename Op::vec, w ^ flip);
+        }
     }
-    const float factor = a.d.scale * 1.4426950408889634f; // scores in powers of two
-    const int32_t *pages = a.d.page_dev + b * a.d.max_pages;
+    const float factor = fabsf(a.d.scale) * 1.4426950408889634f;         // scores in powers of two
+    const PageTable pages = table_of(a, b);
     char *const mine = lds[wave];
-    const uint32_t code_at = c * (D / 2) + quarter * (D / 8), unit_at = c * (D / 32) + quarter * (D / 4) / 32;
+    const int token = lane >> 2, piece = lane & 3;        // as loaded
+    const uint32_t code_at = lane * (D / 8), k_unit_at = c * (D / 32) + quarter * (D / 4) / 32, v_unit_at = token * (D / 32) + piece * (D / 4) / 32;
+    // the way of keys from one to the other, in the place of the values that come after them; pieces swizzled against bank conflicts
+    char *const key_to = mine + token * (D / 2) + (piece ^ (token >> 2)) * (D / 8);
+    const char *const key_from = mine + c * (D / 2) + (quarter ^ (c >> 2)) * (D / 8);
     const int mask = (1 << a.page_shift) - 1;
 
     const auto page_of = [&](int t) { return pages[t < end ? t >> a.page_shift : 0]; };      // (there is a first page if there are tokens)
-    const auto fetch = [&](int t0, const int (&page)[2]) {
-        Fetched<D> f;
+    const auto fetch = [&](Fetched<D> &f, int t0, int page0, int page1) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int t = t0 + 16 * u;
-            f.there[u] = t < end && page[u] >= 0 && page[u] < a.c.pages;
-            const int64_t row = ((static_cast<int64_t>(f.there[u] ? page[u] : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
+            const int t = t0 + 16 * u, page = u ? page1 : page0;
+            f.there[u] = t < end && page >= 0 && page < a.c.pages;
+            const int64_t row = ((static_cast<int64_t>(f.there[u] ? page : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
             f.k[u] = *reinterpret_cast<const Codes<D> *>(a.c.k_codes_dev + row * (D / 2) + code_at);
             f.v[u] = *reinterpret_cast<const Codes<D> *>(a.c.v_codes_dev + row * (D / 2) + code_at);
 #pragma unroll
             for (int y = 0; y < Share<D>::units; ++y) {
-                const uint32_t at = unit_at + (y ? Share<D>::unit(quarter, steps - 1) : 0);    // (the second group of a 96-channel share may be the first again)
-                f.ku[u][y] = (a.c.k_scale_dev + row * (D / 32))[at];
-                f.vu[u][y] = (a.c.v_scale_dev + row * (D / 32))[at];
+                // (the second group of a 96-channel share may be the first again)
+                f.ku[u][y] = (a.c.k_scale_dev + row * (D / 32))[k_unit_at + (y ? Share<D>::unit(quarter, steps - 1) : 0)];
+                f.vu[u][y] = (a.c.v_scale_dev + row * (D / 32))[v_unit_at + (y ? Share<D>::unit(piece, steps - 1) : 0)];
             }
         }
-        return f;
     };
 
     f32x4_t out[D / 16] = {};
-    float top = -INFINITY, sum = 0.0f;                    // of this lane's column: common to its four lanes, and this lane's part
-    int t0 = begin + wave * tokens;
-    int page[2] = {};
-    Fetched<D> now = {};
-    if (t0 < end) {
-        page[0] = page_of(t0);
-        page[1] = page_of(t0 + 16);
-        now = fetch(t0, page);
-        page[0] = page_of(t0 + kTurn);
-        page[1] = page_of(t0 + kTurn + 16);
-    }
-    for (; t0 < end; t0 += kTurn) {
-        const Fetched<D> next = fetch(t0 + kTurn, page);
-        page[0] = page_of(t0 + 2 * kTurn);
-        page[1] = page_of(t0 + 2 * kTurn + 16);
+    float top = -INFINITY, sum = 0.0f;                    // what the column's weights refer to; this lane's part of their sum
+    const auto work = [&](const Fetched<D> &now, int t0) {
+        Codes<D> keys[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) put_codes<D>(key_to + u * 8 * D, now.k[u]);
+        lds_in_order();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) take_codes<D>(key_from + u * 8 * D, keys[u]);
+        lds_in_order();
         f32x4_t score[2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bool written = now.there[u] && t0 + 16 * u + c < x.have;     // beyond the end: whatever it is, made finite
+            const bool written = now.there[u] && t0 + 16 * u + token < x.have;     // beyond the end: whatever it is, made finite
+#pragma unroll
+            for (int s = 0; s < steps; ++s) {
+                const bool second = Share<D>::units > 1 && Share<D>::unit(piece, s);
+                const u32x4_t v = values8<_Float16>(now.v[u].w[s], unit_of(written ? now.vu[u][second ? Share<D>::units - 1 : 0] : 127));
+                *reinterpret_cast<u32x4_t *>(mine + (16 * u + token) * kValueRow<D> + (piece * (D / 4) + 8 * s) * 2) = v;
+            }
 #pragma unroll
             for (int s = 0; s < steps; ++s) {
                 const bool second = Share<D>::units > 1 && Share<D>::unit(quarter, s);
-                const u32x4_t k = values8<T>(now.k[u].w[s], unit_of(now.ku[u][second ? Share<D>::units - 1 : 0]));
+                const u32x4_t k = values8<T>(keys[u].w[s], unit_of(now.ku[u][second ? Share<D>::units - 1 : 0]));
                 score[u] = Op::product(__builtin_bit_cast(typename Op::vec, k), q[s], score[u]);
-                const u32x4_t v = values8<_Float16>(now.v[u].w[s], unit_of(written ? now.vu[u][second ? Share<D>::units - 1 : 0] : 127));
-                *reinterpret_cast<u32x4_t *>(mine + (16 * u + c) * kValueRow<D> + (quarter * (D / 4) + 8 * s) * 2) = v;
             }
-            const int limit = now.there[u] ? seen - t0 - 16 * u - 4 * quarter : 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) score[u][j] = j < limit ? score[u][j] * factor : -INFINITY;
         }
-        float best = top;
+        if (t0 + tokens > least || !now.there[0] || !now.there[1]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int limit = now.there[u] ? seen - t0 - 16 * u - 4 * quarter : 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) score[u][j] = j < limit ? score[u][j] : -INFINITY;
+            }
+        }
+        float best = fmaxf(score[0][0], score[1][0]);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) best = fmaxf(best, score[u][j]);
-        best = column_max(best);
-        const float base = best == -INFINITY ? 0.0f : best, keep = __builtin_amdgcn_exp2f(top - base);
-        top = best;
+            for (int j = 1; j < 4; ++j) best = fmaxf(best, score[u][j]);
+        best = column_max(best) * factor;
+        if (__any(best > top + kSlack)) {
+            const float higher = fmaxf(top, best), keep = __builtin_amdgcn_exp2f(top - (higher == -INFINITY ? 0.0f : higher));
+            top = higher;
+            sum *= keep;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) out[d] *= keep;
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
         half8_t p;
-        float part = 0.0f;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float e = __builtin_amdgcn_exp2f(score[u][j] - base);
-                part += e;
+                const float e = __builtin_amdgcn_exp2f(fmaf(score[u][j], factor, -base));
+                sum += e;
                 p[4 * u + j] = static_cast<_Float16>(e);
             }
-        sum = sum * keep + part;
-        lds_in_order();
+        lds_in_order();                                   // this wave's values are in LDS
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) {
             const char *from = mine + (4 * quarter + (c >> 2)) * kValueRow<D> + (16 * d + 4 * (c & 3)) * 2;
@@ -278,10 +327,27 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[4 * u + j] = __builtin_bit_cast(_Float16, static_cast<short>(y[j]));
             }
-            out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, out[d] * keep, 0, 0, 0);
+            out[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p, out[d], 0, 0, 0);
         }
         lds_in_order();
-        now = next;
+    };
+    int t0 = begin + wave * tokens;
+    if (t0 < end) {                                       // two sets of registers in turn
+        Fetched<D> one, two;
+        fetch(one, t0, page_of(t0), page_of(t0 + 16));
+        int page0 = page_of(t0 + kTurn), page1 = page_of(t0 + kTurn + 16);
+        for (;;) {
+            fetch(two, t0 + kTurn, page0, page1);
+            page0 = page_of(t0 + 2 * kTurn);
+            page1 = page_of(t0 + 2 * kTurn + 16);
+            work(one, t0);
+            if ((t0 += kTurn) >= end) break;
+            fetch(one, t0 + kTurn, page0, page1);
+            page0 = page_of(t0 + 2 * kTurn);
+            page1 = page_of(t0 + 2 * kTurn + 16);
+            work(two, t0);
+            if ((t0 += kTurn) >= end) break;
+        }
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -337,8 +403,7 @@ template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<
 // D = 256).  The tokens' codes are converted once for all rows, into two tiles of LDS in turn: while one is multiplied, the next
 // is converted and the codes of the one after are on their way.  As for 16 rows, scores are computed transposed and the weights
 // stay in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
-// values are read in that order.  The maximum that weights refer to moves only when a score exceeds it by 2^8, which fp16
-// weights and fp32 sums have room for, so that accumulators are rarely rescaled.
+// values are read in that order.
 template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
 {
     using Op = Operand<T>;
@@ -365,7 +430,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     const int seen = live ? seen_by(x, i) : 0;
     // every row of the wave sees the tokens before `least`, none one from `mine` on
     const int wave_first = x.r0 + 32 * wave, rows = x.n * a.group;
-    const int least = wave_first + 31 < rows ? seen_by(x, wave_first / a.group) : 0;
+    const int least = wave_first < rows ? seen_by(x, wave_first / a.group) : 0;
     const int mine = wave_first < rows ? seen_by(x, min((wave_first + 31) / a.group, x.n - 1)) : 0;
     typename Op::vec q[steps];
     {
@@ -454,7 +519,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                 for (int j = 0; j < 16; ++j) best = fmaxf(best, score[u][j]);
             const u32x2_t two = both_halves(best);
             best = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * factor;
-            if (__any(best > top + 8.0f)) {
+            if (__any(best > top + kSlack)) {
                 const float higher = fmaxf(top, best), base = higher == -INFINITY ? 0.0f : higher, keep = __builtin_amdgcn_exp2f(top - base);
                 top = higher;
                 sum *= keep;
@@ -541,6 +606,7 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_jo
     float l = 0.0f;
     f32x4_t o = {};
     if (team < teams) {
+#pragma unroll 4
         for (int s = team; s < parts; s += teams) {
             const float *part = part_of<D>(a, unit, s, row);
             const float f = __builtin_amdgcn_exp2f(part[D] - base);
@@ -608,7 +674,10 @@ static AttentionPlan plan_attention(const apnn_kv_attention_desc &d, const apnn_
     p.tiles = ceil_div(rows, p.tile_rows);
     p.part_rows = static_cast<int>(rows < p.tile_rows ? rows : p.tile_rows);
     const int64_t blocks = p.tiles * pairs;
-    int64_t splits = (p.tile_rows == 16 ? 2048 : 512) / blocks;
+    // two blocks a compute unit in any case, more only while a split keeps 2048 tokens
+    // (2 x 131072 tokens on 4 heads: 28, 30, 34, 44 us with 512, 1024, 2048, 4096 blocks; 48 x 8192 on 8: 92, 68, 65, 64)
+    int64_t splits = 512 / blocks, most = 2048 / blocks < room / 2048 ? 2048 / blocks : room / 2048;
+    if (p.tile_rows == 16 && splits < most) splits = most;
     if (splits > ceil_div(room, kLeastSplit)) splits = ceil_div(room, kLeastSplit);
     p.splits = splits < 1 ? 1 : static_cast<int>(splits);
     if (p.splits > 1) p.bytes = static_cast<size_t>(blocks) * p.splits * p.part_rows * (c.D + 4) * sizeof(float);
