@@ -372,22 +372,14 @@ def apnn_quantize_tokens(src: torch.Tensor, codes: Optional[torch.Tensor] = None
                          scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """src: rows x K (float32, float16 or bfloat16; any row stride) -> int8 codes [rows][apnn_token_pitch(K)] and fp32 scales
     [rows], row = codes * scale.  Activations of a call, and weights (output channels x K) once."""
-    if codes is None:
-        codes = torch.empty((src.shape[0], -(-src.shape[1] // 16) * 16), dtype=torch.int8, device=src.device)
-    if scale is None:
-        scale = torch.empty(src.shape[0], dtype=torch.float32, device=src.device)
-    _N.quantize_tokens(src, codes, scale)
-    return codes, scale
+    return _N.quantize_tokens(src, codes, scale)
 
 
 def apnn_gemm_scaled(X: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, K: int, *,
                      bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X: M x K, W: N x K codes as apnn_quantize_tokens lays them out -> M x N of `dtype` (or into `out`, of any row stride)."""
-    if out is None:
-        out = torch.empty((X.shape[0], W.shape[0]), dtype=dtype, device=X.device)
-    _N.gemm_scaled(X, x_scale, W, w_scale, K, bias, out)
-    return out
+    return _N.gemm_scaled(X, x_scale, W, w_scale, K, bias, out, dtype)
 
 
 @dataclass
@@ -422,17 +414,12 @@ def apnn_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torc
     """k, v: tokens x heads x D into the cache's slots (int64, page * page_size + place; negative: padding, left out).
     table (fp32, positions x rot: cosines, then sines) and positions (int32) rotate the first rot channels of keys and of q
     (tokens x query heads x D).  Returns the rotated queries (q_out, which may be q itself; made if not given), None without q."""
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _N.kv_append(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, k, v, slots, positions, table, interleaved, q, q_out)
-    return q_out
+    return _N.kv_append(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, k, v, slots, positions, table, interleaved, q, q_out)
 
 
 def apnn_kv_read(cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
     """The keys and values that slots (int64) hold, each len(slots) x heads x D; zeros for slots outside the cache."""
-    k, v = (torch.empty((slots.shape[0], cache.heads, cache.D), dtype=dtype, device=slots.device) for _ in range(2))
-    _N.kv_read(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, slots, k, v)
-    return k, v
+    return _N.kv_read(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, slots, dtype)
 
 
 def apnn_kv_attention_workspace_bytes(cache: KVCache, tokens: int, q_heads: int, seqs: int, max_pages: int, *,
@@ -449,12 +436,7 @@ def apnn_kv_attention(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, pages
     sequence's queries begin (None: one query each); max_q: a bound on the queries of a sequence (default: all of them,
     which is right but spreads the work for one sequence that has them all).  Rows of `out` that no sequence has are left as
     they were.  workspace: uint8, for the caller to keep (default: allocated for the call)."""
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if max_q is None:
-        max_q = q.shape[0] if q_start is not None else 1
-    _N.kv_attention(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
-    return out
+    return _N.kv_attention(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
 
 
 def apnn_fold_bn(gamma, beta, mean, var, eps: float, zero: float, step: float):

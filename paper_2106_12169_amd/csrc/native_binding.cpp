@@ -12,6 +12,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -463,6 +464,29 @@ public:
     }
     at::Device device() const { return device_; }
 
+    // A result: the next argument, or where it is None a new tensor, contiguous, of these sizes and type.
+    at::Tensor result(const char *name, at::IntArrayRef want, at::ScalarType type, bool dense)
+    {
+        if (!ok_) return {};
+        if (a_[i_] == Py_None) {
+            ++i_;
+            return at::empty(want, at::TensorOptions().dtype(type).device(device_));
+        }
+        const at::Tensor *t = strided(name, static_cast<int>(want.size()));
+        if (!t) return {};
+        if (t->scalar_type() != type) fail(PyExc_TypeError, "%s: type %s is expected, got %s", name, c10::toString(type), c10::toString(t->scalar_type()));
+        if (ok_ && dense && !t->is_contiguous()) fail(PyExc_AssertionError, "%s: a contiguous tensor is expected", name);
+        sizes(name, t, want);
+        return *t;
+    }
+    // Whether the next argument is None; it is passed over if so.
+    bool none()
+    {
+        if (!ok_ || a_[i_] != Py_None) return false;
+        ++i_;
+        return true;
+    }
+
     // Calls the library on the tensors' device: f(stream).
     template <class F> PyObject *call(F &&f)
     {
@@ -491,26 +515,48 @@ private:
 
 template <class T> T *data(const at::Tensor *t) { return t ? static_cast<T *>(t->data_ptr()) : nullptr; }
 
-PyObject *py_quantize_tokens(PyObject *, PyObject *const *args, Py_ssize_t n)   // (src, codes, scale)
+// None, or what a call that succeeded returns.
+PyObject *returned(PyObject *none, const at::Tensor &t)
+{
+    if (!none) return nullptr;
+    Py_DECREF(none);
+    return THPVariable_Wrap(t);
+}
+PyObject *returned(PyObject *none, const at::Tensor &t, const at::Tensor &u)
+{
+    if (!none) return nullptr;
+    Py_DECREF(none);
+    PyObject *pair = PyTuple_New(2), *x = THPVariable_Wrap(t), *y = THPVariable_Wrap(u);
+    if (!pair || !x || !y) {
+        Py_XDECREF(pair);
+        Py_XDECREF(x);
+        Py_XDECREF(y);
+        return nullptr;
+    }
+    PyTuple_SET_ITEM(pair, 0, x);
+    PyTuple_SET_ITEM(pair, 1, y);
+    return pair;
+}
+
+PyObject *py_quantize_tokens(PyObject *, PyObject *const *args, Py_ssize_t n)   // (src, codes or None, scale or None) -> (codes, scale)
 {
     Tensors a(args, n, 3);
-    const at::Tensor *src = a.strided("src", 2), *codes = a.dense("codes", 2, at::kChar), *scale = a.dense("scale", 1, at::kFloat);
+    const at::Tensor *src = a.strided("src", 2);
     const apnn_dtype type = a.type("src", src);
     if (!a.ok()) return nullptr;
     const int64_t rows = src->size(0), K = src->size(1), ld = rows > 1 ? src->stride(0) : K;
-    a.sizes("codes", codes, {rows, apnn_token_pitch(K)});
-    a.sizes("scale", scale, {rows});
+    const at::Tensor codes = a.result("codes", {rows, apnn_token_pitch(K)}, at::kChar, true), scale = a.result("scale", {rows}, at::kFloat, true);
     if (!a.ok()) return nullptr;
-    return a.call([&](void *st) { return apnn_quantize_tokens(data<void>(src), type, rows, K, ld, data<int8_t>(codes), data<float>(scale), st); });
+    return returned(a.call([&](void *st) { return apnn_quantize_tokens(data<void>(src), type, rows, K, ld, data<int8_t>(&codes), data<float>(&scale), st); }), codes, scale);
 }
 
-PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)       // (X, x_scale, W, w_scale, K, bias, out)
+// (X, x_scale, W, w_scale, K, bias, out or None, dtype of a new result) -> out
+PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    Tensors a(args, n, 7);
+    Tensors a(args, n, 8);
     const at::Tensor *X = a.dense("X", 2, at::kChar), *xs = a.dense("x_scale", 1, at::kFloat), *W = a.dense("W", 2, at::kChar), *ws = a.dense("w_scale", 1, at::kFloat);
     const int64_t K = a.integer();
-    const at::Tensor *bias = a.dense("bias", 1, at::kFloat, true), *out = a.strided("out", 2);
-    const apnn_dtype type = a.type("out", out);
+    const at::Tensor *bias = a.dense("bias", 1, at::kFloat, true);
     if (!a.ok()) return nullptr;
     const int64_t M = X->size(0), N = W->size(0), pitch = apnn_token_pitch(K);
     a.sizes("X", X, {M, pitch});
@@ -518,12 +564,22 @@ PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)       
     a.sizes("x_scale", xs, {M});
     a.sizes("w_scale", ws, {N});
     a.sizes("bias", bias, {N});
-    a.sizes("out", out, {M, N});
     if (!a.ok()) return nullptr;
-    const int64_t ldy = M > 1 ? out->stride(0) : N;
-    return a.call([&](void *st) {
-        return apnn_gemm_scaled(data<int8_t>(X), data<float>(xs), data<int8_t>(W), data<float>(ws), data<float>(bias), data<void>(out), type, M, N, K, ldy, st);
-    });
+    at::Tensor out;
+    if (a.none()) {
+        PyObject *type = a.object();
+        if (!THPDtype_Check(type)) a.fail(PyExc_TypeError, "dtype: a torch.dtype is expected");
+        else out = at::empty({M, N}, at::TensorOptions().dtype(reinterpret_cast<THPDtype *>(type)->scalar_type).device(a.device()));
+    } else if (const at::Tensor *given = a.strided("out", 2)) {
+        out = *given;
+        a.sizes("out", given, {M, N});
+    }
+    const apnn_dtype type = a.type("out", &out);
+    if (!a.ok()) return nullptr;
+    const int64_t ldy = M > 1 ? out.stride(0) : N;
+    return returned(a.call([&](void *st) {
+        return apnn_gemm_scaled(data<int8_t>(X), data<float>(xs), data<int8_t>(W), data<float>(ws), data<float>(bias), data<void>(&out), type, M, N, K, ldy, st);
+    }), out);
 }
 
 // the four arrays of a binding.KVCache
@@ -549,7 +605,7 @@ apnn_kv_cache read_cache(Tensors &a)
     return c;
 }
 
-// (k_codes, k_scale, v_codes, v_scale, k, v, slots, positions, table, interleaved, q, q_out)
+// (k_codes, k_scale, v_codes, v_scale, k, v, slots, positions, table, interleaved, q or None, q_out or None) -> q_out, None without q
 PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     Tensors a(args, n, 12);
@@ -557,22 +613,24 @@ PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
     const at::Tensor *k = a.strided("k", 3), *v = a.strided("v", 3), *slots = a.dense("slots", 1, at::kLong);
     const at::Tensor *positions = a.dense("positions", 1, at::kInt, true), *table = a.dense("table", 2, at::kFloat, true);
     const long long interleaved = a.integer();
-    const at::Tensor *q = a.strided("q", 3, true), *q_out = a.strided("q_out", 3, true);
+    const at::Tensor *q = a.strided("q", 3, true);
     apnn_kv_tokens t = {};
     t.type = a.type("k", k);
     a.same_type("v", v, k);
     a.same_type("q", q, k);
-    a.same_type("q_out", q_out, k);
     if (!a.ok()) return nullptr;
     t.tokens = k->size(0);
     a.sizes("k", k, {t.tokens, c.heads, c.D});
     a.sizes("v", v, {t.tokens, c.heads, c.D});
     a.sizes("slots", slots, {t.tokens});
     a.sizes("positions", positions, {t.tokens});
-    if (!q != !q_out || !table != !positions) a.fail(PyExc_ValueError, "q goes with q_out, and positions with a table");
+    if (!table != !positions) a.fail(PyExc_ValueError, "positions go with a table, and a table with positions");
+    at::Tensor q_out;
     if (q) {
         a.sizes("q", q, {t.tokens, q->size(1), c.D});
-        a.sizes("q_out", q_out, {t.tokens, q->size(1), c.D});
+        q_out = a.result("q_out", {t.tokens, q->size(1), c.D}, q->scalar_type(), false);
+    } else if (!a.none()) {
+        a.fail(PyExc_ValueError, "q_out goes with q");
     }
     if (!a.ok()) return nullptr;
     t.k_dev = data<void>(k);
@@ -590,30 +648,32 @@ PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
     if (q && q->size(1)) {
         t.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
         t.q_dev = data<void>(q);
-        t.q_out_dev = data<void>(q_out);
+        t.q_out_dev = data<void>(&q_out);
         t.q_token_stride = q->stride(0); t.q_head_stride = q->stride(1);
-        t.q_out_token_stride = q_out->stride(0); t.q_out_head_stride = q_out->stride(1);
+        t.q_out_token_stride = q_out.stride(0); t.q_out_head_stride = q_out.stride(1);
     }
-    return a.call([&](void *st) { return apnn_kv_append(&c, &t, st); });
+    PyObject *none = a.call([&](void *st) { return apnn_kv_append(&c, &t, st); });
+    return q ? returned(none, q_out) : none;
 }
 
-PyObject *py_kv_read(PyObject *, PyObject *const *args, Py_ssize_t n)           // (k_codes, k_scale, v_codes, v_scale, slots, k_out, v_out)
+PyObject *py_kv_read(PyObject *, PyObject *const *args, Py_ssize_t n)           // (k_codes, k_scale, v_codes, v_scale, slots, dtype) -> (k, v)
 {
-    Tensors a(args, n, 7);
+    Tensors a(args, n, 6);
     const apnn_kv_cache c = read_cache(a);
-    const at::Tensor *slots = a.dense("slots", 1, at::kLong), *k = a.strided("k_out", 3, true), *v = a.strided("v_out", 3, true);
-    const apnn_dtype type = a.type("k_out", k ? k : v);
-    a.same_type("v_out", v, k);
+    const at::Tensor *slots = a.dense("slots", 1, at::kLong);
     if (!a.ok()) return nullptr;
+    PyObject *type = a.object();
+    if (!THPDtype_Check(type)) a.fail(PyExc_TypeError, "dtype: a torch.dtype is expected");
+    if (!a.ok()) return nullptr;
+    const auto options = at::TensorOptions().dtype(reinterpret_cast<THPDtype *>(type)->scalar_type).device(a.device());
     const int64_t count = slots->size(0);
-    a.sizes("k_out", k, {count, c.heads, c.D});
-    a.sizes("v_out", v, {count, c.heads, c.D});
-    if (a.ok() && ((k && !k->is_contiguous()) || (v && !v->is_contiguous()))) a.fail(PyExc_AssertionError, "k_out and v_out: contiguous tensors are expected");
+    const at::Tensor k = at::empty({count, c.heads, c.D}, options), v = at::empty({count, c.heads, c.D}, options);
+    const apnn_dtype as = a.type("dtype", &k);
     if (!a.ok()) return nullptr;
-    return a.call([&](void *st) { return apnn_kv_read(&c, data<int64_t>(slots), count, data<void>(k), data<void>(v), type, st); });
+    return returned(a.call([&](void *st) { return apnn_kv_read(&c, data<int64_t>(slots), count, data<void>(&k), data<void>(&v), as, st); }), k, v);
 }
 
-// (k_codes, k_scale, v_codes, v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
+// (k_codes, k_scale, v_codes, v_scale, q, lens, pages, scale, q_start or None, max_q or None, out or None, workspace or None) -> out
 PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     Tensors a(args, n, 12);
@@ -622,24 +682,22 @@ PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     apnn_kv_attention_desc d = {};
     d.scale = a.real();
     const at::Tensor *q_start = a.dense("q_start", 1, at::kInt, true);
-    d.max_q = a.integer();
-    const at::Tensor *out = a.strided("out", 3), *workspace = a.dense("workspace", 1, at::kByte, true);
-    d.type = a.type("q", q);
-    a.same_type("out", out, q);
     if (!a.ok()) return nullptr;
     d.tokens = q->size(0);
     d.seqs = lens->size(0);
     d.max_pages = pages->size(1);
+    d.max_q = a.none() ? (q_start ? d.tokens : 1) : a.integer();
+    d.type = a.type("q", q);
     a.sizes("q", q, {d.tokens, q->size(1), c.D});
-    a.sizes("out", out, {d.tokens, q->size(1), c.D});
     a.sizes("pages", pages, {d.seqs, d.max_pages});
     a.sizes("q_start", q_start, {d.seqs + 1});
+    const at::Tensor out = a.result("out", {d.tokens, q->size(1), c.D}, q->scalar_type(), false), *workspace = a.dense("workspace", 1, at::kByte, true);
     if (!a.ok()) return nullptr;
     d.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
     d.q_dev = data<void>(q);
-    d.out_dev = data<void>(out);
+    d.out_dev = data<void>(&out);
     d.q_token_stride = q->stride(0); d.q_head_stride = q->stride(1);
-    d.out_token_stride = out->stride(0); d.out_head_stride = out->stride(1);
+    d.out_token_stride = out.stride(0); d.out_head_stride = out.stride(1);
     d.q_start_dev = data<int32_t>(q_start);
     d.len_dev = data<int32_t>(lens);
     d.page_dev = data<int32_t>(pages);
@@ -653,7 +711,7 @@ PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
             scratch = own.data_ptr();
         }
     }
-    return a.call([&](void *st) { return apnn_kv_attention(&d, &c, scratch, bytes, st); });
+    return returned(a.call([&](void *st) { return apnn_kv_attention(&d, &c, scratch, bytes, st); }), out);
 }
 
 PyObject *py_kv_attention_workspace(PyObject *, PyObject *const *args, Py_ssize_t n)    // (heads, page_size, D, tokens, q_heads, seqs, max_pages, ragged, max_q)

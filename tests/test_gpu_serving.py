@@ -629,7 +629,7 @@ def test_the_binding_refuses_wrong_tensors():
         B.apnn_kv_append(cache, k, k.half(), slots)
     with pytest.raises(TypeError, match="slots"):
         B.apnn_kv_append(cache, k, k, slots.int())
-    with pytest.raises(ValueError, match="positions with a table"):
+    with pytest.raises(ValueError, match="positions go with a table"):
         B.apnn_kv_append(cache, k, k, slots, positions=at)
     with pytest.raises(B.ApnnError, match="rot = 66"):
         B.apnn_kv_append(cache, k, k, slots, positions=at, table=torch.zeros((4, 66), device="cuda"))
