@@ -391,25 +391,26 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
 // Two lanes that share a column of the 32 x 32 instruction (lane ^ 32).
 __device__ __forceinline__ u32x2_t both_halves(float x) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false); }
 
-// Bytes between rows of keys and values in LDS of the kernel for many rows: fragment reads of 8 key rows, and transposing reads
-// of 64 bytes of 4 value rows, cover all banks.
+// Bytes between rows of keys and values in LDS of the kernel for many rows: of the paddings that fit, the ones with the fewest bank
+// conflicts by the counters.
 template <int D> constexpr int kManyKeyRow = 2 * D + 16;
-template <int D> constexpr int kManyValueRow = D == 96 ? 320 : 2 * D + 64;
+template <int D> constexpr int kManyValueRow = 2 * D + 32;
 template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<D>);
 
 // 128 query rows of one cache head against one split of the sequence, 32 rows a wave, 64 tokens at a time.
 //
-// Bound by the matrix unit and the vector instructions of the softmax, which two blocks on a compute unit overlap (one where
-// D = 256).  The tokens' codes are converted once for all rows, into two tiles of LDS in turn: while one is multiplied, the next
-// is converted and the codes of the one after are on their way.  As for 16 rows, scores are computed transposed and the weights
-// stay in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
+// Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (one where
+// D = 256) overlap: 34 % and 39 % of the cycles with two blocks of two tiles each, 245 us for prompts of up to 2048 tokens on
+// contexts of up to 4096, 32 heads on 8 of D = 128; 222 us (842 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
+// all rows, those of the next tile on their way meanwhile.  As for 16 rows, scores are computed transposed and the weights stay
+// in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
 // values are read in that order.
-template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
+template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
 {
     using Op = Operand<T>;
     constexpr int steps = D / 16, tokens = 64, words = Share<D>::words;
-    extern __shared__ __attribute__((aligned(16))) char many_lds[];      // [2][keys, values], then [2][4] pages that are there
-    uint8_t *const pages_there = reinterpret_cast<uint8_t *>(many_lds + 2 * kManyTile<D>);
+    extern __shared__ __attribute__((aligned(16))) char many_lds[];      // keys, values, then [4] pages that are there
+    uint8_t *const pages_there = reinterpret_cast<uint8_t *>(many_lds + kManyTile<D>);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
     const int64_t id = first + blockIdx.x, unit = SPLIT ? quotient(id, a.splits) : id;
     const int split = SPLIT ? static_cast<int>(id - unit * a.splits) : 0;
@@ -468,32 +469,28 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         }
         return f;
     };
-    const auto convert = [&](const Row &f, int buf) {
-        char *const k_to = many_lds + buf * kManyTile<D> + token * kManyKeyRow<D> + quarter * (D / 2);
-        char *const v_to = many_lds + buf * kManyTile<D> + 64 * kManyKeyRow<D> + token * kManyValueRow<D> + quarter * (D / 2);
+    const auto convert = [&](const Row &f) {
+        char *const k_to = many_lds + token * kManyKeyRow<D> + quarter * (D / 2);
+        char *const v_to = many_lds + 64 * kManyKeyRow<D> + token * kManyValueRow<D> + quarter * (D / 2);
 #pragma unroll
         for (int s = 0; s < words; ++s) {
             const bool second = Share<D>::units > 1 && Share<D>::unit(quarter, s);
             *reinterpret_cast<u32x4_t *>(k_to + 16 * s) = values8<T>(f.k.w[s], unit_of(f.ku[second ? Share<D>::units - 1 : 0]));
             *reinterpret_cast<u32x4_t *>(v_to + 16 * s) = values8<_Float16>(f.v.w[s], unit_of(f.written ? f.vu[second ? Share<D>::units - 1 : 0] : 127));
         }
-        if ((threadIdx.x & 63) == 0) pages_there[4 * buf + token / 16] = f.there;
+        if ((threadIdx.x & 63) == 0) pages_there[token / 16] = f.there;
     };
 
     f32x16_t out[D / 32] = {};
     float top = -INFINITY, sum = 0.0f;                    // what the column's weights refer to; this lane's part of their sum
     Row next = {};
-    if (begin < end) {
-        convert(fetch(begin), 0);
-        next = fetch(begin + tokens);
-    }
-    __syncthreads();
-    for (int t0 = begin, buf = 0; t0 < end; t0 += tokens, buf ^= 1) {
-        const Row later = fetch(t0 + 2 * tokens);
-        convert(next, buf ^ 1);                           // (after the last tile: of nothing that is read)
-        next = later;
+    if (begin < end) next = fetch(begin);
+    for (int t0 = begin; t0 < end; t0 += tokens) {
+        convert(next);
+        next = fetch(t0 + tokens);
+        __syncthreads();
         if (t0 < mine) {
-            const char *const keys = many_lds + buf * kManyTile<D>, *const values = keys + 64 * kManyKeyRow<D>;
+            const char *const keys = many_lds, *const values = keys + 64 * kManyKeyRow<D>;
             f32x16_t score[2] = {};
 #pragma unroll
             for (int s = 0; s < steps; ++s)
@@ -502,7 +499,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                     const u32x4_t k = *reinterpret_cast<const u32x4_t *>(keys + (32 * u + c) * kManyKeyRow<D> + 32 * s + 16 * half);
                     score[u] = Op::product(__builtin_bit_cast(typename Op::vec, k), q[s], score[u]);
                 }
-            const uint32_t there = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t *>(pages_there + 4 * buf));
+            const uint32_t there = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t *>(pages_there));
             if (t0 + tokens > least || there != 0x01010101u) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -733,7 +730,7 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         if (a.tile_rows == 128) {
-            constexpr int bytes = 2 * kManyTile<D> + 16;
+            constexpr int bytes = kManyTile<D> + 16;
             if constexpr (bytes > 64 * 1024) {
                 static std::atomic<uint64_t> granted[2];
                 if (!all_of_lds(kv_attention_many_kernel<T, D, false>, granted[0]) || !all_of_lds(kv_attention_many_kernel<T, D, true>, granted[1]))
