@@ -33,6 +33,11 @@
  *                 these asks for another form)
  *   INPUT_TILE    input layers with the image rows staged once per block: 0 never,
  *                 1 whenever it applies
+ *   SCALED_TILE   apnn_gemm_scaled: 16 the form for few tokens, 64 | 128 | 256 tiles
+ *                 of that edge, 129 the 128-wide ones one block to a compute unit
+ *   KV_ROWS       apnn_kv_attention: 16 | 128 query rows a block (its workspace goes
+ *                 by the value set when it is asked for: a call that needs more
+ *                 then is refused)
  * A forced value the dispatch cannot honour for a call is ignored for that call.
  */
 #ifndef APNN_DEBUG_H

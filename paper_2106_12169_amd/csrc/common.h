@@ -50,8 +50,10 @@ template <class Kernel> bool all_of_lds(Kernel kernel, std::atomic<uint64_t> &gr
     return true;
 }
 
-// Override INPUT_TILE (layer.hip): -1 when it is not set.
+// Overrides INPUT_TILE, SCALED_TILE and KV_ROWS (layer.hip): -1 when they are not set.
 int input_tile_override();
+int scaled_tile_override();
+int kv_rows_override();
 
 inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s); }
 

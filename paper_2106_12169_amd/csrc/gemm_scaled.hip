@@ -292,11 +292,14 @@ template <class T> int launch_scaled(const ScaledGemm &p, hipStream_t st)
         if (wide == 2) return launch_few<T, MT, 2, 4, 1>(p, st);
         return launch_few<T, MT, 1, 4, MT == 4 ? 1 : 2>(p, st);
     };
-    const int wide = static_cast<int>(units / 192);
+    const int wide = static_cast<int>(units / 192), forced = scaled_tile_override();
+    if (forced == 64) return launch_tiles<T, 1, 4>(p, st);
+    if (forced == 128 || forced == 129) return forced == 128 ? launch_tiles<T, 2, 2>(p, st) : launch_tiles<T, 2, 4>(p, st);
+    if (forced == 256) return launch_tiles<T, 4, 2>(p, st);
     if (p.M <= 16) return launch_few<T, 1, 1, 4, 2>(p, st);
     if (p.M <= 32) return few(std::integral_constant<int, 2>{}, wide);
     if (p.M <= 48) return few(std::integral_constant<int, 3>{}, wide);
-    if (p.M <= 64) return few(std::integral_constant<int, 4>{}, wide);
+    if (p.M <= 64 || forced == 16) return few(std::integral_constant<int, 4>{}, wide);
     // A few more: 64 tokens a block while that is about one block a compute unit and reads nothing often
     // (M = 256, N = 1000, K = 1999: 7.6 us, 64 x 64 tiles 9.6; M = 128, N = K = 4096: 10.3, 11.6; M = 200: 13.6, 12.1).
     const int64_t down = ceil_div(p.M, 64);

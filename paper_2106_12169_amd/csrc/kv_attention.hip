@@ -6,6 +6,7 @@
 // (ds_read_b64_tr_b16).  A 4-bit group with its power of two is exact in 16 bits, so the conversion
 // (v_cvt_scalef32_pk_*_fp4, two values an instruction) costs no accuracy: keys take the queries' type, values fp16.
 #include "kv_cache.h"
+#include "lane_util.h"
 #include "lds_load.h"
 
 namespace apnn {
@@ -399,16 +400,16 @@ template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<
 
 // 128 query rows of one cache head against one split of the sequence, 32 rows a wave, 64 tokens at a time.
 //
-// Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (one where
+// Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (two where
 // D = 256) overlap: 34 % and 39 % of the cycles with two blocks of two tiles each, 245 us for prompts of up to 2048 tokens on
-// contexts of up to 4096, 32 heads on 8 of D = 128; 222 us (842 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
+// contexts of up to 4096, 32 heads on 8 of D = 128; 223 us (840 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
 // all rows, those of the next tile on their way meanwhile.  As for 16 rows, scores are computed transposed and the weights stay
 // in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
 // values are read in that order.
-template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
+template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_many_kernel(AttentionArgs a, int64_t first)
 {
     using Op = Operand<T>;
-    constexpr int steps = D / 16, tokens = 64, words = Share<D>::words;
+    constexpr int steps = D / 16, tokens = 64, words = Share<D>::words, kAhead = 2;
     extern __shared__ __attribute__((aligned(16))) char many_lds[];      // keys, values, then [4] pages that are there
     uint8_t *const pages_there = reinterpret_cast<uint8_t *>(many_lds + kManyTile<D>);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5;
@@ -452,9 +453,10 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     // loader: thread 4 t + u has token t of a tile and channels [D / 4 u, + D / 4)
     const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
     struct Row { Codes<D> k, v; uint8_t ku[Share<D>::units], vu[Share<D>::units]; bool there, written; };
-    const auto fetch = [&](int t0) {
+    const auto page_of = [&](int t0) { return t0 + token < end ? pages[(t0 + token) >> a.page_shift] : -1; };
+    const auto fetch = [&](int t0, int page) {
         Row f;
-        const int t = t0 + token, page = pages[t < end ? t >> a.page_shift : 0];         // (tokens there are, so there is a first page)
+        const int t = t0 + token;
         f.there = t < end && page >= 0 && page < a.c.pages;
         f.written = f.there && t < x.have;
         const int64_t row = ((static_cast<int64_t>(f.there ? page : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
@@ -484,30 +486,55 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     f32x16_t out[D / 32] = {};
     float top = -INFINITY, sum = 0.0f;                    // what the column's weights refer to; this lane's part of their sum
     Row next = {};
-    if (begin < end) next = fetch(begin);
+    int page = -1;
+    if (begin < end) {
+        next = fetch(begin, page_of(begin));
+        page = page_of(begin + tokens);
+    }
     for (int t0 = begin; t0 < end; t0 += tokens) {
         convert(next);
-        next = fetch(t0 + tokens);
+        next = fetch(t0 + tokens, page);
+        page = page_of(t0 + 2 * tokens);                  // (a page number is there by the time its codes are asked for)
         __syncthreads();
         if (t0 < mine) {
             const char *const keys = many_lds, *const values = keys + 64 * kManyKeyRow<D>;
+            // fragments are read kAhead instructions before they are multiplied (left to itself the compiler waits for each)
             f32x16_t score[2] = {};
+            const auto key = [&](auto ic) {
+                constexpr int i = decltype(ic)::value;    // step i / 2, tokens 32 (i % 2) ..
+                return __builtin_bit_cast(typename Op::vec, *reinterpret_cast<const u32x4_t *>(keys + (32 * (i % 2) + c) * kManyKeyRow<D> + 32 * (i / 2) + 16 * half));
+            };
+            typename Op::vec k[kAhead];
+            static_for<kAhead>([&](auto i) { k[i] = key(i); });
+            static_for<2 * steps>([&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                score[i % 2] = Op::product(k[i % kAhead], q[i / 2], score[i % 2]);
+                if constexpr (i + kAhead < 2 * steps) k[i % kAhead] = key(std::integral_constant<int, i + kAhead>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            const auto value = [&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i / (D / 32), d = i % (D / 32);       // tokens 16 s .., channels 32 d ..
+                const char *from = values + (16 * s + 4 * half + (lane % 16 >> 2)) * kManyValueRow<D> + (32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4)) * 2;
+                half8_t v;
 #pragma unroll
-            for (int s = 0; s < steps; ++s)
+                for (int h = 0; h < 2; ++h) {
+                    const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(from + 8 * h * kManyValueRow<D>));
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const u32x4_t k = *reinterpret_cast<const u32x4_t *>(keys + (32 * u + c) * kManyKeyRow<D> + 32 * s + 16 * half);
-                    score[u] = Op::product(__builtin_bit_cast(typename Op::vec, k), q[s], score[u]);
+                    for (int j = 0; j < 4; ++j) v[4 * h + j] = __builtin_bit_cast(_Float16, static_cast<short>(y[j]));
                 }
+                return v;
+            };
+            half8_t v[kAhead];
+            static_for<kAhead>([&](auto i) { v[i] = value(i); });
             const uint32_t there = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t *>(pages_there));
             if (t0 + tokens > least || there != 0x01010101u) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int g = 0; g < 4; ++g) {             // 16 tokens, of one page
+                    const int limit = there >> (8 * g) & 1 ? seen - t0 - 16 * g - 4 * half : INT_MIN;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const bool page = there >> (16 * u + 8 * (j / 8)) & 1;
-                        if (!(page && t0 + 32 * u + 8 * (j / 4) + 4 * half + j % 4 < seen)) score[u][j] = -INFINITY;
-                    }
+                    for (int j = 0; j < 8; ++j)
+                        if (8 * (j / 4) + j % 4 >= limit) score[g / 2][8 * (g % 2) + j] = -INFINITY;
+                }
             }
             float best = score[0][0];
 #pragma unroll
@@ -535,20 +562,13 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                     sum += e;
                     p[2 * u + j / 8][j % 8] = static_cast<_Float16>(e);
                 }
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d) {
-                    const char *from = values + (16 * s + 4 * half + (lane % 16 >> 2)) * kManyValueRow<D> + (32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4)) * 2;
-                    half8_t v;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)(from + 8 * h * kManyValueRow<D>));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[4 * h + j] = __builtin_bit_cast(_Float16, static_cast<short>(y[j]));
-                    }
-                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[s], out[d], 0, 0, 0);
-                }
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<D / 8>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i / (D / 32), d = i % (D / 32);
+                out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i % kAhead], p[s], out[d], 0, 0, 0);
+                if constexpr (i + kAhead < D / 8) v[i % kAhead] = value(std::integral_constant<int, i + kAhead>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
         }
         __syncthreads();
     }
@@ -581,13 +601,17 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         }
 }
 
-// Joins the splits' parts of one row, a block a row: D / 4 lanes take its channels, the others further splits.
-template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a, int64_t first)
+// Joins the splits' parts of a row: D / 4 lanes take its channels.  Where rows are few and splits many, a block takes one row and
+// its teams of lanes further splits of it; else every team a row of its own.
+template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a, int64_t first)
 {
     constexpr int lanes = D / 4, teams = 256 / lanes;
-    __shared__ f32x4_t sums[teams][lanes];
+    __shared__ f32x4_t sums[MANY ? 1 : teams][lanes];
     __shared__ float weights[teams];
-    const int64_t id = first + blockIdx.x, unit = quotient(id, a.part_rows);
+    const int team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    if (MANY && team >= teams) return;
+    const int64_t id = MANY ? (first + blockIdx.x) * teams + team : first + blockIdx.x, unit = quotient(id, a.part_rows);
+    if (MANY && unit >= a.tiles * a.d.seqs * a.c.heads) return;
     const int row = static_cast<int>(id - unit * a.part_rows);
     const Place place = place_of(a, unit);
     const int head = place.head;
@@ -595,33 +619,42 @@ template <class T, int D> __global__ __launch_bounds__(256) void kv_attention_jo
     const int rr = x.r0 + row, ri = rr / a.group;
     if (!x.any || ri >= x.n) return;
     const int each = split_tokens(x.most, a.splits), parts = max(1, (x.most + each - 1) / each);
-    float m = -INFINITY;
-    for (int s = threadIdx.x & 63; s < parts; s += 64) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float base = m == -INFINITY ? 0.0f : m;
-    const int team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    float l = 0.0f;
+    float l = 0.0f, m = -INFINITY;
     f32x4_t o = {};
+    if (MANY) {
+        for (int s = 0; s < parts; ++s) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
+    } else {
+        for (int s = threadIdx.x & 63; s < parts; s += 64) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
+        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
     if (team < teams) {
 #pragma unroll 4
-        for (int s = team; s < parts; s += teams) {
+        for (int s = MANY ? 0 : team; s < parts; s += MANY ? 1 : teams) {
             const float *part = part_of<D>(a, unit, s, row);
             const float f = __builtin_amdgcn_exp2f(part[D] - base);
             l += part[D + 1] * f;
             o += *reinterpret_cast<const f32x4_t *>(part + 4 * lane) * f;
         }
-        sums[team][lane] = o;
-        if (lane == 0) weights[team] = l;
     }
-    __syncthreads();
-    if (team) return;
-    for (int s = 1; s < teams; ++s) {
-        o += sums[s][lane];
-        l += weights[s];
+    if constexpr (!MANY) {
+        if (team < teams) {
+            sums[team][lane] = o;
+            if (lane == 0) weights[team] = l;
+        }
+        __syncthreads();
+        if (team) return;
+        for (int s = 1; s < teams; ++s) {
+            o += sums[s][lane];
+            l += weights[s];
+        }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + 4 * lane;
-    for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
+    T y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(o[j] * inv);
+    __builtin_memcpy(to, y, sizeof y);
 }
 
 }  // namespace apnn
@@ -667,7 +700,12 @@ static AttentionPlan plan_attention(const apnn_kv_attention_desc &d, const apnn_
     p.max_q = d.q_start_dev ? (d.max_q < d.tokens ? d.max_q : d.tokens) : 1;
     if (d.tokens == 0 || d.seqs == 0 || p.max_q == 0) return p;
     const int64_t rows = p.max_q * group, pairs = static_cast<int64_t>(c.heads) * d.seqs, room = d.max_pages * c.page_size;
-    p.tile_rows = rows >= 64 ? 128 : 16;
+    // 128 rows a block pay where blocks are enough without splits, or scores many (us, 16 and 128 rows; 32 heads on 8, D = 128: 1 x 256 queries
+    // on 2048 tokens 24, 34; 1 x 1024 60, 57; 1 x 2048 80, 59; 4 x 1024 on 1024 95, 54; 1 x 128 on 32768 152, 104; 16 heads, D = 64: 1 x 2048
+    // on 2048 26, 35; 8 x 500 on 500 24, 15)
+    const bool many = rows >= 64 && (ceil_div(rows, 128) * pairs >= 384 || static_cast<double>(rows) * pairs * (room - p.max_q / 2) >= 4e7);
+    const int forced = kv_rows_override();
+    p.tile_rows = forced == 16 || forced == 128 ? forced : (many ? 128 : 16);
     p.tiles = ceil_div(rows, p.tile_rows);
     p.part_rows = static_cast<int>(rows < p.tile_rows ? rows : p.tile_rows);
     const int64_t blocks = p.tiles * pairs;
@@ -743,8 +781,11 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
         } else {
             sliced(units * a.splits, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         }
-        if (a.splits > 1)
-            sliced(units * a.part_rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
+        const int64_t rows = units * a.part_rows;
+        if (a.splits > 1 && rows >= 2048)
+            sliced(ceil_div(rows, 256 / (D / 4)), [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
+        else if (a.splits > 1)
+            sliced(rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D, false><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         return check_launch(who);
     };
     return by_channels(cache->D, [&](auto d) { return desc->type == APNN_F16 ? go(_Float16{}, d) : go(__bf16{}, d); });

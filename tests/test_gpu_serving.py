@@ -133,6 +133,24 @@ def test_gemm_scaled(M, N, K):
         check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=b, dtype=dtype), X, xs, W, ws, b, dtype)
 
 
+@pytest.mark.parametrize("form", [16, 64, 128, 129, 256])
+@pytest.mark.parametrize("M, N, K", [(1, 1, 1), (5, 33, 300), (65, 70, 16), (130, 513, 129), (257, 255, 640), (300, 1000, 1999), (513, 256, 4096)])
+def test_gemm_scaled_in_every_form(M, N, K, form):
+    X, xs, W, ws, bias = operands(M, N, K, low=-128)
+    B.apnn_debug_force("SCALED_TILE", form)
+    for dtype, b in ((F32, bias), (F16, None), (BF16, bias)):
+        check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=b, dtype=dtype), X, xs, W, ws, b, dtype)
+    ws[N // 2], xs[M // 2] = 1e-30, 1e25                  # scales that cannot be multiplied as they are
+    check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, dtype=F32), X, xs, W, ws, None, F32)
+
+
+def test_gemm_scaled_large():
+    """Sizes that choose the widest tiles by themselves, whole rounds of them and a part of one."""
+    for M, N, K in ((4096, 4096, 320), (4000, 4100, 144)):
+        X, xs, W, ws, bias = operands(M, N, K)
+        check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=bias, dtype=BF16), X, xs, W, ws, bias, BF16)
+
+
 def test_gemm_scaled_at_the_edge_of_int32():
     K = (1 << 17) - 1
     X = torch.full((3, B.apnn_token_pitch(K)), -128, dtype=torch.int8, device="cuda")
@@ -352,6 +370,12 @@ def check_attention(out, q, cache, table, lens, news, starts, scale, dtype):
             close(out[rows, h], want, dtype, error[:, None] * spread + l * 2.0 ** -25 * big)
 
 
+@pytest.fixture(params=[16, 128], ids=["rows16", "rows128"])
+def rows(request):
+    """Both kernels, whatever the sizes would choose."""
+    B.apnn_debug_force("KV_ROWS", request.param)
+
+
 def attend(seed, lens, news, Hq, heads, D, page, dtype, ragged=None, scale=None, max_q=None):
     g = rng(seed)
     cache, table = filled(g, lens, heads, page, D)
@@ -373,24 +397,24 @@ def attend(seed, lens, news, Hq, heads, D, page, dtype, ragged=None, scale=None,
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
 @pytest.mark.parametrize("Hq, heads", [(1, 1), (3, 3), (4, 1), (14, 2), (16, 1), (40, 2)])
-def test_attention_of_single_tokens(D, Hq, heads, dtype):
+def test_attention_of_single_tokens(D, Hq, heads, dtype, rows):
     attend(D + Hq, [1, 16, 17, 100, 333, 0, 31, 32, 33, 64], [1] * 10, Hq, heads, D, 16, dtype)
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
-def test_attention_of_every_page_size(page):
+def test_attention_of_every_page_size(page, rows):
     attend(page, [page - 1, page, page + 1, 3 * page + 5], [1] * 4, 8, 2, 64, page, F16)
     attend(page + 1, [page - 1, page, page + 1, 3 * page + 5], [5, page, 40, 2 * page], 4, 2, 128, page, BF16)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("D, Hq, heads", [(64, 4, 4), (96, 6, 2), (128, 8, 2), (128, 7, 1), (256, 4, 1)])
-def test_attention_of_prompts(D, Hq, heads, dtype):
+def test_attention_of_prompts(D, Hq, heads, dtype, rows):
     attend(D * 3 + Hq, [70, 257, 1, 130, 40, 0, 200], [70, 100, 1, 129, 3, 0, 200], Hq, heads, D, 32, dtype)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
-def test_attention_rows_that_see_nothing(dtype):
+def test_attention_rows_that_see_nothing(dtype, rows):
     """More queries than tokens: the first ones stand before the cache begins and get zeros."""
     _, _, _, out = attend(3, [3, 0, 40, 1], [10, 5, 45, 200], 4, 2, 64, 16, dtype)
     assert (out[:7] == 0).all() and (out[7:10] != 0).any()
@@ -398,19 +422,19 @@ def test_attention_rows_that_see_nothing(dtype):
 
 
 @pytest.mark.parametrize("news", [1, 2, 3, 4, 8, 16])
-def test_attention_of_a_few_tokens_on_long_contexts(news):
+def test_attention_of_a_few_tokens_on_long_contexts(news, rows):
     attend(news, [5000, 1200, 4096, 2047], [news, 1, news, news], 16, 2, 128, 64, BF16)
     attend(news + 50, [3000], [news], 8, 8, 64, 16, F16)
 
 
-def test_attention_scales_and_far_scores():
+def test_attention_scales_and_far_scores(rows):
     """Scores far apart, negative scale, scale 0 (plain averages); one token with all of the weight."""
     for scale in (-0.3, 0.0, 3.0, 1e-30):
         attend(11, [300, 20], [1, 1], 4, 2, 64, 16, F16, scale=scale)
         attend(12, [300, 150], [100, 150], 4, 2, 64, 16, BF16, scale=scale)
 
 
-def test_attention_max_q_and_one_query_each():
+def test_attention_max_q_and_one_query_each(rows):
     cache, table, q, out = attend(21, [50, 60, 70], [1, 1, 1], 4, 2, 64, 16, F16, ragged=False)
     lens = torch.tensor([50, 60, 70], dtype=torch.int32, device="cuda")
     start = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
@@ -427,7 +451,7 @@ def test_attention_max_q_and_one_query_each():
 
 
 @pytest.mark.parametrize("news", [1, 40])
-def test_attention_nan_reaches_only_queries_that_see_it(news):
+def test_attention_nan_reaches_only_queries_that_see_it(news, rows):
     g, D, page, l = rng(news), 64, 16, 200
     cache, table = filled(g, [l], 2, page, D)
     bad = l - max(1, news // 2)                           # seen by the later half of the queries
@@ -448,7 +472,7 @@ def test_attention_nan_reaches_only_queries_that_see_it(news):
 
 
 @pytest.mark.parametrize("news", [1, 30])
-def test_attention_skips_pages_outside_the_cache(news):
+def test_attention_skips_pages_outside_the_cache(news, rows):
     """A page index out of range counts as unseen, wherever it stands; so do tokens beyond the table."""
     g, D, page, l = rng(4), 128, 32, 300
     cache, table = filled(g, [l, l], 2, page, D)
@@ -472,7 +496,7 @@ def test_attention_skips_pages_outside_the_cache(news):
 
 
 @pytest.mark.parametrize("news", [1, 70])
-def test_attention_strides(news):
+def test_attention_strides(news, rows):
     g, D, Hq, H = rng(9), 64, 4, 2
     cache, table = filled(g, [200], H, 16, D)
     for odd in (0, 1):
@@ -487,13 +511,19 @@ def test_attention_strides(news):
         assert (whole == 9.0).all()
 
 
-def test_attention_of_many_sequences():
+def test_attention_that_chooses_many_rows_itself():
+    """Enough blocks of 128 rows, and enough scores, for that kernel to be taken (and joined from splits)."""
+    attend(61, [150] * 64, [100] * 64, 8, 8, 64, 16, BF16)
+    attend(62, [9000, 40], [260, 40], 32, 2, 64, 64, F16)
+
+
+def test_attention_of_many_sequences(rows):
     lens = [(37 * b) % 90 for b in range(300)]
     attend(31, lens, [1] * 300, 2, 1, 64, 16, BF16)
     attend(32, lens[:60], [min(l, b % 5) for b, l in enumerate(lens[:60])], 2, 1, 64, 16, F16)
 
 
-def test_attention_beyond_32_bits_of_offset():
+def test_attention_beyond_32_bits_of_offset(rows):
     """Pages whose bytes start past 2^32: a cache of 5 GB a side, most of it unused."""
     D, page, heads = 256, 256, 8
     pages = (5 << 30) // (heads * page * D // 2)
