@@ -151,32 +151,43 @@ template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ?
         lds_in_order();
         const char *from_lds = mine + lane / LANES * ROW + lane % LANES * V * 4;
         const float *x = x_scale + 32 * b + lane / LANES;
-        int m = mw + 32 * b + lane / LANES;
-        T *to = static_cast<T *>(p.Y) + m * p.ldy + n;
+        constexpr int DOWN = 64 / LANES;                  // rows that lie between two of a lane's
+        const auto leave = [&](int i, const T (&y)[V]) {
+            const int m = mw + 32 * b + lane / LANES + i;
+            T *const to = static_cast<T *>(p.Y) + m * p.ldy + n;
+            if (m < p.M && n + V <= p.N) __builtin_memcpy(to, y, sizeof y);          // (wherever a row begins)
+            else if (m < p.M)
+#pragma unroll
+                for (int j = 0; j < V - 1; ++j)
+                    if (n + j < p.N) to[j] = y[j];
+        };
+        if (far) {
 #pragma unroll 1
-        for (int i = 0; i < 32; i += 128 / LANES) {       // two rows a lane in a turn
-            i32x4_t sum[2][V / 4];
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int j = 0; j < V / 4; ++j) sum[u][j] = *reinterpret_cast<const i32x4_t *>(from_lds + (i + u * (64 / LANES)) * ROW + 16 * j);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const float xs = x[i + u * (64 / LANES)];
+            for (int i = 0; i < 32; i += DOWN) {
                 T y[V];
-                if (far)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) y[j] = static_cast<T>(scaled(sum[u][j / 4][j % 4], scale_of(xs), scale_of(w[j]), bias[j]));
-                else
+                for (int j = 0; j < V; ++j) y[j] = static_cast<T>(scaled(reinterpret_cast<const int *>(from_lds + i * ROW)[j], scale_of(x[i]), scale_of(w[j]), bias[j]));
+                leave(i, y);
+            }
+        } else {
+            constexpr int AT_ONCE = 32 / DOWN < 4 ? 32 / DOWN : 4;
+#pragma unroll 1
+            for (int i = 0; i < 32; i += AT_ONCE * DOWN) {
+                i32x4_t sum[AT_ONCE][V / 4];
+                float xs[AT_ONCE];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) y[j] = static_cast<T>(static_cast<float>(sum[u][j / 4][j % 4]) * xs * w[j] + bias[j]);
-                if (m < p.M && n + V <= p.N) __builtin_memcpy(to, y, sizeof y);      // (wherever a row begins)
-                else if (m < p.M)
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    xs[u] = x[i + u * DOWN];
 #pragma unroll
-                    for (int j = 0; j < V - 1; ++j)
-                        if (n + j < p.N) to[j] = y[j];
-                m += 64 / LANES;
-                to += 64 / LANES * p.ldy;
+                    for (int j = 0; j < V / 4; ++j) sum[u][j] = *reinterpret_cast<const i32x4_t *>(from_lds + (i + u * DOWN) * ROW + 16 * j);
+                }
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    T y[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[j] = static_cast<T>(static_cast<float>(sum[u][j / 4][j % 4]) * xs[u] * w[j] + bias[j]);
+                    leave(i + u * DOWN, y);
+                }
             }
         }
         lds_in_order();

@@ -28,47 +28,64 @@ struct AppendArgs {
     int page_shift;
 };
 
-// (a, b) turned: a cos - b sin, b cos + a sin, in 64 bits, rounded once.
-__device__ __forceinline__ void turn(float &a, float &b, float cs, float sn)
-{
-    const double x = a, y = b, c = cs, s = sn;
-    a = static_cast<float>(x * c - y * s);
-    b = static_cast<float>(y * c + x * s);
-}
+// What the rotation makes of channels c0 .. c0 + 7 of a row, in 64 bits, rounded once.
+struct Rotation {
+    enum Kind { NONE, PAIRS, HALVES, ODD } kind;          // not reached; pairs of neighbours; halves of 8 channels in a row; else
+    int c0, rot;
+    __device__ __forceinline__ Rotation(int c, int r, bool interleaved) : kind(c >= r ? NONE : interleaved ? PAIRS : r % 16 == 0 ? HALVES : ODD), c0(c), rot(r) {}
+    __device__ __forceinline__ int half() const { return rot >> 1; }
+    __device__ __forceinline__ bool first() const { return c0 < half(); }
+    __device__ __forceinline__ int other() const { return first() ? c0 + half() : c0 - half(); }     // HALVES: where the pairs' other halves begin
+};
 
-// Channels c0 .. c0 + 7 of a row, rotated where the rotation reaches them.
-template <class T> __device__ __forceinline__ void rotated8(const T *x, int c0, int rot, bool interleaved, const float *angles, float (&y)[8])
+// y: the channels; z: the other halves of their pairs (HALVES); angles: rot / 2 cosines, rot / 2 sines.
+template <class T> __device__ __forceinline__ void rotate(const Rotation &r, const T *x, const float *angles, float (&y)[8], const float (&z)[8])
 {
-    load8(x + c0, y);
-    if (c0 >= rot) return;
-    const int half = rot >> 1;
-    if (interleaved) {                                    // four pairs, some of them perhaps beyond the rotation
+    const int half = r.half();
+    if (r.kind == Rotation::PAIRS) {
+        // four pairs; where the rotation ends among them, the angles of the last four, moved up, and none
+        const int i = min(r.c0 >> 1, max(half - 4, 0)), by = (r.c0 >> 1) - i;
+        float cs[4], sn[4];
+        if (half >= 4) {
+            __builtin_memcpy(cs, angles + i, 16);
+            __builtin_memcpy(sn, angles + half + i, 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                cs[j] = j < half ? angles[j] : 1.0f;
+                sn[j] = j < half ? angles[half + j] : 0.0f;
+            }
+        }
+        if (by) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = j + by;
+                cs[j] = k < 4 ? (k == 1 ? cs[1] : k == 2 ? cs[2] : cs[3]) : 1.0f;
+                sn[j] = k < 4 ? (k == 1 ? sn[1] : k == 2 ? sn[2] : sn[3]) : 0.0f;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int i = (c0 >> 1) + j;
-            if (i < half) turn(y[2 * j], y[2 * j + 1], angles[i], angles[half + i]);
+            const double a = y[2 * j], b = y[2 * j + 1], c = cs[j], d = sn[j];
+            const bool reached = (r.c0 >> 1) + j < half;  // (what is not keeps its value, whatever its neighbour is)
+            y[2 * j] = reached ? static_cast<float>(a * c - b * d) : y[2 * j];
+            y[2 * j + 1] = reached ? static_cast<float>(b * c + a * d) : y[2 * j + 1];
         }
-    } else if (half % 8 == 0) {                           // the pairs' other halves are eight channels in a row, too
-        float z[8], cs[8], sn[8];
-        const bool first = c0 < half;
-        const int i = first ? c0 : c0 - half;
-        load8(x + (first ? c0 + half : i), z);
+    } else if (r.kind == Rotation::HALVES) {
+        float cs[8], sn[8];
+        const int i = r.first() ? r.c0 : r.other();
         load8(angles + i, cs);
         load8(angles + half + i, sn);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float a = first ? y[j] : z[j], b = first ? z[j] : y[j];
-            turn(a, b, cs[j], sn[j]);
-            y[j] = first ? a : b;
-        }
-    } else {
+        for (int j = 0; j < 8; ++j)
+            y[j] = static_cast<float>(static_cast<double>(y[j]) * cs[j] + static_cast<double>(z[j]) * (r.first() ? -sn[j] : sn[j]));
+    } else if (r.kind == Rotation::ODD) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int c = c0 + j, i = c < half ? c : c - half;
-            if (c >= rot) continue;
-            float a = c < half ? y[j] : static_cast<float>(x[i]), b = c < half ? static_cast<float>(x[c + half]) : y[j];
-            turn(a, b, angles[i], angles[half + i]);
-            y[j] = c < half ? a : b;
+            const int c = r.c0 + j, i = c < half ? c : c - half;
+            if (c >= r.rot) continue;
+            const double own = y[j], pair = static_cast<float>(x[c < half ? c + half : i]), cs = angles[i], sn = angles[half + i];
+            y[j] = static_cast<float>(own * cs + pair * (c < half ? -sn : sn));
         }
     }
 }
@@ -103,48 +120,45 @@ __device__ __forceinline__ bool finite8(const float (&y)[8])
 }
 
 // TEAM lanes (the power of two that holds D / 8) take one row: of a cache head, key and value, or of a query head.
+//
+// Bound by vector instructions (64 % of the cycles; the rotation's conversions to and from 64 bits lead) and by the way from a
+// token's slot and position to its angles: what does not wait for the position is asked for at once, angles are read 16 bytes at a
+// time.  8000 tokens, 8 cache and 32 query heads of D = 64, half of the channels rotated in neighbouring pairs: 22 us; four heads
+// a team, with a quarter of the look-ups, 52.
 template <class T, int D, int TEAM> __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a, int64_t first)
 {
     const int64_t item = first + static_cast<int64_t>(blockIdx.x) * (256 / TEAM) + threadIdx.x / TEAM;
-    const int heads = a.c.heads + a.t.q_heads, part = threadIdx.x % TEAM, c0 = part * 8;
+    const int heads = a.c.heads + a.t.q_heads, part = threadIdx.x % TEAM;
+    const bool mine = part * 8 < D;
+    const int c0 = mine ? part * 8 : 0;
     const int64_t token = quotient(item, heads);
     const int h = static_cast<int>(item - token * heads);
-    bool live = token < a.t.tokens && c0 < D;
-    int64_t slot = 0;
-    const float *angles = nullptr;
-    if (live) {
-        slot = a.t.slot_dev[token];
-        live = slot >= 0 && slot < a.c.pages << a.page_shift;
-        if (a.t.rot) {
-            const int64_t at = a.t.position_dev[token];
-            live = live && at >= 0 && at < a.t.table_rows;
-            angles = a.t.table_dev + (live ? at : 0) * a.t.rot;
-        }
-    }
-    float y[8] = {};
-    if (h >= a.c.heads) {                                 // (a team has one item, so it leaves together)
-        if (!live) return;
-        const int64_t hq = h - a.c.heads;
-        const T *q = static_cast<const T *>(a.t.q_dev) + token * a.t.q_token_stride + hq * a.t.q_head_stride;
-        rotated8(q, c0, a.t.rot, a.t.interleaved, angles, y);
-        T *out = static_cast<T *>(a.t.q_out_dev) + token * a.t.q_out_token_stride + hq * a.t.q_out_head_stride + c0;
-        __builtin_amdgcn_wave_barrier();                  // in place: every lane of the team has read its pairs
-        store8(y, out);
+    if (token >= a.t.tokens) return;                      // (a whole team, as below)
+    const bool is_query = h >= a.c.heads;
+    const Rotation r(c0, a.t.rot, a.t.interleaved);
+    const T *x = is_query ? static_cast<const T *>(a.t.q_dev) + token * a.t.q_token_stride + (h - a.c.heads) * a.t.q_head_stride
+                          : static_cast<const T *>(a.t.k_dev) + token * a.t.k_token_stride + h * a.t.k_head_stride;
+    const int64_t slot = a.t.slot_dev[token], at = a.t.rot ? a.t.position_dev[token] : 0;
+    float y[8], z[8] = {}, v[8] = {};
+    load8(x + c0, y);
+    if (r.kind == Rotation::HALVES) load8(x + r.other(), z);
+    if (!is_query) load8(static_cast<const T *>(a.t.v_dev) + token * a.t.v_token_stride + h * a.t.v_head_stride + c0, v);
+    __builtin_amdgcn_sched_barrier(0);
+    if (slot < 0 || slot >= a.c.pages << a.page_shift || at < 0 || (a.t.rot && at >= a.t.table_rows)) return;
+    rotate(r, x, a.t.table_dev + at * a.t.rot, y, z);
+    if (is_query) {
+        __builtin_amdgcn_wave_barrier();                  // in place: every lane of the team, all of one wave, has read its pairs
+        if (mine) store8(y, static_cast<T *>(a.t.q_out_dev) + token * a.t.q_out_token_stride + (h - a.c.heads) * a.t.q_out_head_stride + c0);
         return;
     }
-    float z[8] = {};
-    if (live) {
-        rotated8(static_cast<const T *>(a.t.k_dev) + token * a.t.k_token_stride + h * a.t.k_head_stride, c0, a.t.rot, a.t.interleaved, angles, y);
-        load8(static_cast<const T *>(a.t.v_dev) + token * a.t.v_token_stride + h * a.t.v_head_stride + c0, z);
-    }
-    int bad = !(finite8(y) && finite8(z));
+    int bad = !(finite8(y) && finite8(v));
     for (int d = 1; d < TEAM; d <<= 1) bad |= __shfl_xor(bad, d);
     if (bad)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = z[j] = 0.0f;
+        for (int j = 0; j < 8; ++j) y[j] = v[j] = 0.0f;
     int ky, vy;
-    const uint32_t kw = codes8(y, ky), vw = codes8(z, vy);
-    if (!live) return;
+    const uint32_t kw = codes8(y, ky), vw = codes8(v, vy);
+    if (!mine) return;
     const int64_t row = cache_row(slot, h, a.c.heads, a.page_shift);
     reinterpret_cast<uint32_t *>(a.c.k_codes_dev)[row * (D / 8) + part] = kw;
     reinterpret_cast<uint32_t *>(a.c.v_codes_dev)[row * (D / 8) + part] = vw;

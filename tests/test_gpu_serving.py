@@ -276,6 +276,23 @@ def test_append_borders_between_codes():
         np.testing.assert_array_equal(f64(B.apnn_kv_read(cache, torch.arange(T, device="cuda"), out)[0]), want.k[:T])
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [2, 6, 12, 20, 30, 48])
+def test_append_rotates_nothing_beyond_the_rotation(rot, interleaved):
+    """Channels from rot on keep their values, next to infinities too."""
+    D, T = 64, 5
+    cache, g = B.KVCache.empty(1, 1, 16, D), rng(rot)
+    q = normal(g, T, 3, D, dtype=BF16)
+    q[:, :, rot + 1::4] = float("inf")
+    k = normal(g, T, 1, D, dtype=BF16)
+    table = rotation(rot, 50)
+    positions = torch.arange(T, dtype=torch.int32, device="cuda") * 9
+    out = B.apnn_kv_append(cache, k, k, torch.arange(T, device="cuda"), positions=positions, table=torch.from_numpy(table).cuda(), interleaved=interleaved, q=q)
+    want = O.rotate(f64(q), table, positions.cpu().numpy(), interleaved)
+    assert torch.equal(out[:, :, rot:], q[:, :, rot:])
+    close(out[:, :, :rot], want[:, :, :rot], BF16)
+
+
 def test_append_holds_what_is_not_finite_as_nan():
     g, D = rng(5), 128
     k, v = normal(g, 6, 2, D), normal(g, 6, 2, D)
