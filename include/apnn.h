@@ -334,7 +334,7 @@ typedef struct {
     int64_t table_rows;
     const int32_t *position_dev;/* [tokens] */
     /* Queries rotated like the keys and written to q_out; q_heads 0: none.
-     * q_out may be q itself, with the same strides. */
+     * q_out may be q itself, with the same strides; otherwise they must not overlap. */
     int q_heads;
     const void *q_dev;          /* [tokens][q_heads][D] */
     void *q_out_dev;

@@ -676,6 +676,8 @@ int check_attention(const char *who, const apnn_kv_attention_desc *d, const apnn
     if (d->q_heads >= c->heads && d->tokens * (d->q_heads / c->heads) > (int64_t(1) << 30))
         return fail(APNN_ERR_UNSUPPORTED, "%s: %lld rows of %d heads for each cache head", who, (long long)d->tokens, d->q_heads / c->heads);
     if (d->q_heads < 1 || d->q_heads % c->heads) return fail(APNN_ERR_INVALID_ARG, "%s: %d query heads over %d cache heads", who, d->q_heads, c->heads);
+    const double rows = static_cast<double>(d->q_start_dev ? (d->max_q < d->tokens ? d->max_q : d->tokens) : 1) * d->q_heads;
+    if ((rows / 16 + c->heads) * d->seqs > 1e12) return fail(APNN_ERR_UNSUPPORTED, "%s: %lld sequences of up to %lld queries", who, (long long)d->seqs, (long long)d->max_q);
     if (!(d->scale - d->scale == 0.0f)) return fail(APNN_ERR_INVALID_ARG, "%s: scale is not finite", who);
     if (!d->q_start_dev && d->tokens < d->seqs) return fail(APNN_ERR_INVALID_ARG, "%s: one query each for %lld sequences, %lld rows", who, (long long)d->seqs, (long long)d->tokens);
     return APNN_OK;
@@ -740,6 +742,7 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
     const AttentionPlan plan = plan_attention(*desc, *cache);
     if (plan.tiles == 0) return APNN_OK;
     if (!desc->q_dev || !desc->out_dev || !desc->len_dev || (desc->max_pages && !desc->page_dev)) return fail(APNN_ERR_INVALID_ARG, "%s: null pointer", who);
+    if (desc->q_dev == desc->out_dev) return fail(APNN_ERR_INVALID_ARG, "%s: out must not be q", who);
     if (!aligned_to(desc->q_dev, desc->type) || !aligned_to(desc->out_dev, desc->type)) return fail(APNN_ERR_ALIGNMENT, "%s: a pointer is not aligned to its type", who);
     if (!strides_fit(desc->tokens, desc->q_heads, cache->D, desc->q_token_stride, desc->q_head_stride, false) ||
         !strides_fit(desc->tokens, desc->q_heads, cache->D, desc->out_token_stride, desc->out_head_stride, true))

@@ -124,7 +124,7 @@ extern "C" int apnn_quantize_tokens(const void *src_dev, apnn_dtype type, int64_
     clear_error();
     if (!known_type(type)) return fail(APNN_ERR_INVALID_ARG, "apnn_quantize_tokens: unknown type %d", static_cast<int>(type));
     if (rows < 0 || K < 0 || ld < K) return fail(APNN_ERR_INVALID_ARG, "apnn_quantize_tokens: rows = %lld, K = %lld, ld = %lld", (long long)rows, (long long)K, (long long)ld);
-    if (K > INT_MAX - 1024) return fail(APNN_ERR_UNSUPPORTED, "apnn_quantize_tokens: K = %lld", (long long)K);
+    if (K > (int64_t(1) << 30)) return fail(APNN_ERR_UNSUPPORTED, "apnn_quantize_tokens: K = %lld", (long long)K);
     if (rows && ld > INT64_MAX / 8 / rows) return fail(APNN_ERR_INVALID_ARG, "apnn_quantize_tokens: %lld rows of stride %lld", (long long)rows, (long long)ld);
     if (rows == 0) return APNN_OK;
     if ((K && (!src_dev || !codes_dev)) || !scale_dev) return fail(APNN_ERR_INVALID_ARG, "apnn_quantize_tokens: null pointer");

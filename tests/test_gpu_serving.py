@@ -528,6 +528,36 @@ def test_attention_strides(news, rows):
         assert (whole == 9.0).all()
 
 
+def test_attention_with_a_workspace_that_is_kept():
+    """One workspace for call after call, of the size asked for; and one that is too small is refused."""
+    g, D = rng(79), 64
+    cache, table = filled(g, [5000, 4000], 2, 64, D)
+    need = B.apnn_kv_attention_workspace_bytes(cache, 2, 8, 2, table.shape[1])
+    space = torch.full((need + 32,), 255, dtype=torch.uint8, device="cuda")
+    for l in ([5000, 4000], [1, 3000], [0, 5]):
+        q, lens = normal(g, 2, 8, D, dtype=F16), torch.tensor(l, dtype=torch.int32, device="cuda")
+        out = B.apnn_kv_attention(cache, q, lens, table, 0.125, workspace=space[:need])
+        assert torch.equal(out, B.apnn_kv_attention(cache, q, lens, table, 0.125))
+        check_attention(out, q, cache, table, l, [1, 1], [0, 1], 0.125, F16)
+    assert (space[need:] == 255).all()
+    with pytest.raises(B.ApnnError, match="workspace"):
+        B.apnn_kv_attention(cache, q, lens, table, 0.125, workspace=space[:need - 1])
+
+
+@pytest.mark.parametrize("news", [1, 33])
+def test_attention_of_queries_that_share_memory(news, rows):
+    """One query row for all heads and tokens (strides 0) is only read; the result has memory of its own."""
+    g, D = rng(80), 96
+    cache, table = filled(g, [150], 2, 16, D)
+    q = normal(g, 1, 1, D, dtype=BF16).expand(news, 6, D)
+    start = torch.tensor([0, news], dtype=torch.int32, device="cuda")
+    out = B.apnn_kv_attention(cache, q, torch.tensor([150], dtype=torch.int32, device="cuda"), table, 0.1, q_start=start, max_q=news)
+    check_attention(out, q, cache, table, [150], [news], [0], 0.1, BF16)
+    own = normal(g, news, 6, D, dtype=BF16)
+    with pytest.raises(B.ApnnError, match="out must not be q"):
+        B.apnn_kv_attention(cache, own, torch.tensor([150], dtype=torch.int32, device="cuda"), table, 0.1, q_start=start, max_q=news, out=own)
+
+
 def test_attention_that_chooses_many_rows_itself():
     """Enough blocks of 128 rows, and enough scores, for that kernel to be taken (and joined from splits)."""
     attend(61, [150] * 64, [100] * 64, 8, 8, 64, 16, BF16)

@@ -28,7 +28,7 @@ def tokens(**over):
 
 
 def attention(**over):
-    d = dict(tokens=3, type=2, q_heads=4, q_dev=FAKE, out_dev=FAKE, q_token_stride=256, q_head_stride=64, out_token_stride=256, out_head_stride=64,
+    d = dict(tokens=3, type=2, q_heads=4, q_dev=FAKE, out_dev=FAKE + 4096, q_token_stride=256, q_head_stride=64, out_token_stride=256, out_head_stride=64,
              seqs=3, q_start_dev=None, len_dev=FAKE, page_dev=FAKE, max_pages=2, max_q=1, scale=1.0)
     d.update(over)
     return B.KVAttentionDesc(**d)
@@ -114,6 +114,8 @@ def test_read_refusals(status, args):
     (UNSUPPORTED, dict(type=0)), (UNSUPPORTED, dict(type=3)), (ARG, dict(tokens=-1)), (ARG, dict(seqs=-1)), (ARG, dict(max_pages=-1)), (ARG, dict(max_q=-1)),
     (ARG, dict(q_heads=3)), (ARG, dict(q_heads=0)), (ARG, dict(scale=float("inf"))), (ARG, dict(scale=float("nan"))), (ARG, dict(seqs=4)),
     (ARG, dict(q_dev=None)), (ARG, dict(out_dev=None)), (ARG, dict(len_dev=None)), (ARG, dict(page_dev=None)), (ALIGNMENT, dict(q_dev=FAKE + 1)),
+    (ARG, dict(out_dev=FAKE)), (UNSUPPORTED, dict(max_pages=1 << 27)), (UNSUPPORTED, dict(tokens=1 << 30, q_start_dev=FAKE, max_q=1 << 20, seqs=1 << 30)),
+    (UNSUPPORTED, dict(tokens=(1 << 30) + 1, q_heads=2, q_start_dev=FAKE)), (ARG, dict(max_pages=4096)),       # (the last one: a workspace is needed)
     (ARG, dict(out_head_stride=0)), (ARG, dict(out_token_stride=64)), (ARG, dict(q_token_stride=-256)),
     (0, dict(seqs=0)), (0, dict(tokens=0, seqs=0)), (0, dict(max_q=0, q_start_dev=FAKE)),
 ])
@@ -122,6 +124,21 @@ def test_attention_refusals(status, over):
     assert bool(last()) == bool(status)
     assert B.lib().apnn_kv_attention(None, C.byref(cache()), None, 0, None) == ARG
     assert B.lib().apnn_kv_attention(C.byref(attention()), None, None, 0, None) == ARG
+
+
+def test_workspace_sizes():
+    """Splits of long contexts where blocks are few, and none where they are many or contexts short."""
+    c = B.KVCache.empty(2, 2, 16, 64, "cpu")
+    size = B.apnn_kv_attention_workspace_bytes
+    assert size(c, 1, 4, 1, 64) == 0                                    # 1024 tokens
+    assert size(c, 1, 4, 1, 4096) % ((64 + 4) * 4) == 0 and size(c, 1, 4, 1, 4096) > 0
+    assert size(c, 5000, 4, 5000, 4096) == 0
+    assert size(c, 0, 4, 0, 4096) == 0
+    L, d = B.lib(), attention(max_pages=4096)
+    need = L.apnn_kv_attention_workspace_bytes(C.byref(d), C.byref(cache()))
+    assert need > 0
+    assert L.apnn_kv_attention(C.byref(d), C.byref(cache()), FAKE, need - 1, None) == ARG and "workspace" in last()
+    assert L.apnn_kv_attention(C.byref(d), C.byref(cache()), FAKE + 8, need, None) == ALIGNMENT
 
 
 def test_the_binding_refuses_what_is_no_device_tensor():
