@@ -21,6 +21,8 @@
  *   - `stream` is the caller's hipStream_t passed as void* (NULL = the null
  *     stream).  Calls validate their arguments on the host, enqueue their
  *     kernels on that stream and return without synchronising.
+ *   - No entry point needs scratch memory but apnn_kv_attention, whose caller
+ *     provides it.
  *   - Every function returning int returns an apnn_status; on failure nothing
  *     has been enqueued and apnn_last_error() (thread local) says why.
  *   - Packed buffers must be 16-byte aligned (APNN_ERR_ALIGNMENT otherwise).
@@ -191,7 +193,7 @@ int apnn_layer(const apnn_layer_desc *desc, const uint32_t *W_dev, const uint32_
 /* Device scratch memory apnn_layer / apnn_layer_pair / apnn_input_layer would
  * need for `desc`, for the caller to allocate: always 0.  Every reduction of the
  * kernels (K split over the waves of a block, the row-sum term of Sec. 3.2
- * Case III) happens in registers and LDS, so no entry point takes a workspace. */
+ * Case III) happens in registers and LDS. */
 size_t apnn_workspace_bytes(const apnn_layer_desc *desc);
 
 /* Two layers that do not depend on each other (neither reads what the other
