@@ -607,7 +607,7 @@ template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_a
 {
     constexpr int lanes = D / 4, teams = 256 / lanes;
     __shared__ f32x4_t sums[MANY ? 1 : teams][lanes];
-    __shared__ float weights[teams];
+    __shared__ float tops[teams], weights[teams];
     const int team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     if (MANY && team >= teams) return;
     const int64_t id = MANY ? (first + blockIdx.x) * teams + team : first + blockIdx.x, unit = quotient(id, a.part_rows);
@@ -621,32 +621,50 @@ template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_a
     const int each = split_tokens(x.most, a.splits), parts = max(1, (x.most + each - 1) / each);
     float l = 0.0f, m = -INFINITY;
     f32x4_t o = {};
-    if (MANY) {
-        for (int s = 0; s < parts; ++s) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
-    } else {
-        for (int s = threadIdx.x & 63; s < parts; s += 64) m = fmaxf(m, part_of<D>(a, unit, s, row)[D]);
-        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    }
-    const float base = m == -INFINITY ? 0.0f : m;
-    if (team < teams) {
-#pragma unroll 4
-        for (int s = MANY ? 0 : team; s < parts; s += MANY ? 1 : teams) {
-            const float *part = part_of<D>(a, unit, s, row);
-            const float f = __builtin_amdgcn_exp2f(part[D] - base);
-            l += part[D + 1] * f;
-            o += *reinterpret_cast<const f32x4_t *>(part + 4 * lane) * f;
+    // four parts asked for at once, each brought to the maximum so far
+    for (int s = MANY ? 0 : team; s < parts; s += 4 * (MANY ? 1 : teams)) {
+        float pm[4], pl[4];
+        f32x4_t po[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int at = s + u * (MANY ? 1 : teams);
+            const float *part = part_of<D>(a, unit, at < parts ? at : s, row);
+            pm[u] = at < parts ? part[D] : -INFINITY;
+            pl[u] = part[D + 1];
+            po[u] = *reinterpret_cast<const f32x4_t *>(part + 4 * lane);
+        }
+        const float higher = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), base = higher == -INFINITY ? 0.0f : higher;
+        const float keep = __builtin_amdgcn_exp2f(m - base);
+        m = higher;
+        l *= keep;
+        o *= keep;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (s + u * (MANY ? 1 : teams) >= parts) continue;
+            const float f = __builtin_amdgcn_exp2f(pm[u] - base);
+            l += pl[u] * f;
+            o += po[u] * f;
         }
     }
     if constexpr (!MANY) {
         if (team < teams) {
             sums[team][lane] = o;
-            if (lane == 0) weights[team] = l;
+            if (lane == 0) {
+                weights[team] = l;
+                tops[team] = m;
+            }
         }
         __syncthreads();
         if (team) return;
-        for (int s = 1; s < teams; ++s) {
-            o += sums[s][lane];
-            l += weights[s];
+        float top = -INFINITY;
+        for (int s = 0; s < teams; ++s) top = fmaxf(top, tops[s]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        o = f32x4_t{};
+        l = 0.0f;
+        for (int s = 0; s < teams; ++s) {
+            const float f = __builtin_amdgcn_exp2f(tops[s] - base);
+            o += sums[s][lane] * f;
+            l += weights[s] * f;
         }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -785,7 +803,7 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
             sliced(units * a.splits, [&](int64_t first, unsigned blocks) { kv_attention_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         }
         const int64_t rows = units * a.part_rows;
-        if (a.splits > 1 && rows >= 2048)
+        if (a.splits > 1 && (rows >= 2048 || a.splits <= 8))
             sliced(ceil_div(rows, 256 / (D / 4)), [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D, true><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
         else if (a.splits > 1)
             sliced(rows, [&](int64_t first, unsigned blocks) { kv_attention_join_kernel<T, D, false><<<blocks, 256, 0, as_stream(stream)>>>(a, first); });
