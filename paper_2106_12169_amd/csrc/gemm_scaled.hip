@@ -53,7 +53,8 @@ __device__ __forceinline__ void tile_of(const ScaledGemm &p, int id, int &tm, in
 // The sums leave through LDS, 32 tokens at a time (a store to LDS takes them from the accumulators' half of the register file
 // as they are), to lanes that keep the same channels for all tokens: those channels' scales stay in registers, and a lane
 // stores 16 bytes.  Its code is a loop: unrolled over the accumulators it was 72 KB that every launch fetched anew: 17 us of
-// 4096 x 4096 outputs where this takes 14.
+// 4096 x 4096 outputs where this takes 13.  4096^3 in 65 us: 26 ns a matrix instruction with random codes, 17.6 with zeros, as the
+// clock gives way to the power the products take.
 template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void gemm_scaled_tile_kernel(ScaledGemm p)
 {
     constexpr int EDGE = 64 * F, CHUNK = 128, SIDE = EDGE * CHUNK, STEPS = CHUNK / 32, LOADS = 2 * F;   // loads of a wave, chunk and operand
@@ -197,7 +198,7 @@ template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ?
 // Few tokens: 16 MT tokens x 16 NT channels a block, the block's waves sharing K in turns of 128 bytes.
 //
 // Bound by reading W once.  Lanes of a fragment read straight from memory lie a row apart, which costs the address unit four
-// times as long as neighbours do (M = 40, N = 10240, K = 5120: 35 us), so a wave brings its turns through LDS: eight
+// times as long as neighbours do (M = 40, N = 10240, K = 5120: 35 us; 13.5 as it is), so a wave brings its turns through LDS: eight
 // neighbours load a whole 128-byte line of a row, its pieces swizzled by row for the fragment reads.  A wave has LDS of its own, STAGES turns
 // of it in flight, and waits for nobody before the sums are joined.  X comes from L2 for each block: MT / NT bytes for each
 // byte of W; rows beyond M are out of the buffer's range and cost nothing.
@@ -307,7 +308,8 @@ template <class T> int launch_scaled(const ScaledGemm &p, hipStream_t st)
     if (forced == 64) return launch_tiles<T, 1, 4>(p, st);
     if (forced == 128 || forced == 129) return forced == 128 ? launch_tiles<T, 2, 2>(p, st) : launch_tiles<T, 2, 4>(p, st);
     if (forced == 256) return launch_tiles<T, 4, 2>(p, st);
-    if (p.M <= 16) return launch_few<T, 1, 1, 4, 2>(p, st);
+    // (one token, N = 1000: K = 12000 7.4 us with four waves a block, 5.7 with eight; K = 4096 3.9, 3.8; K = 1000 2.8, 3.0)
+    if (p.M <= 16) return p.pitch >= 8192 ? launch_few<T, 1, 1, 8, 2>(p, st) : launch_few<T, 1, 1, 4, 2>(p, st);
     if (p.M <= 32) return few(std::integral_constant<int, 2>{}, wide);
     if (p.M <= 48) return few(std::integral_constant<int, 3>{}, wide);
     if (p.M <= 64 || forced == 16) return few(std::integral_constant<int, 4>{}, wide);

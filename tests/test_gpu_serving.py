@@ -123,7 +123,7 @@ def check_product(got, X, xs, W, ws, bias, dtype):
 
 SIZES = [(1, 1, 1), (1, 64, 64), (1, 4096, 1024), (2, 100, 31), (5, 33, 4096), (16, 64, 16), (17, 48, 48), (31, 257, 640), (33, 1000, 500),
          (48, 512, 2048), (64, 128, 1000), (65, 129, 257), (100, 77, 20000), (128, 128, 128), (200, 333, 111), (257, 255, 4096),
-         (512, 512, 64), (777, 1000, 1999), (1024, 1024, 1024), (300, 2048, 4112), (2049, 2047, 33), (4096, 24, 512), (3, 9000, 7000)]
+         (512, 512, 64), (777, 1000, 1999), (1024, 1024, 1024), (300, 2048, 4112), (2049, 2047, 33), (4096, 24, 512), (3, 9000, 7000), (1, 40, 9000), (16, 100, 12001)]
 
 
 @pytest.mark.parametrize("M, N, K", SIZES)
