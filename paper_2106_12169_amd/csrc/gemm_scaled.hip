@@ -21,6 +21,7 @@ struct ScaledGemm {
     int64_t ldy;
     int M, N, pitch;                                      // pitch: bytes of a row of X and W
     int across, tiles;                                    // tiles of a row of tiles, of the result
+    bool stream;                                          // the result is too large to wait in L2 for its reader
 };
 
 struct Scale {
@@ -52,8 +53,9 @@ __device__ __forceinline__ void tile_of(const ScaledGemm &p, int id, int &tm, in
 //
 // The sums leave through LDS, 32 tokens at a time (a store to LDS takes them from the accumulators' half of the register file
 // as they are), to lanes that keep the same channels for all tokens: those channels' scales stay in registers, and a lane
-// stores 16 bytes.  Its code is a loop: unrolled over the accumulators it was 72 KB that every launch fetched anew: 17 us of
-// 4096 x 4096 outputs where this takes 13.  4096^3 in 65 us: 26 ns a matrix instruction with random codes, 17.6 with zeros, as the
+// stores 16 bytes, past L2 where the result is 16 MiB or more (33 MB: 18.1 us without the products, 13.9 so; 16.8 MB: 13.3, 10.9;
+// 8.4 MB: 9.3, 8.8, left to L2 for its reader).  Its code is a loop: unrolled over the accumulators it was 72 KB that every launch fetched anew: 17 us of
+// 4096 x 4096 outputs where this takes 9.  4096^3 in 64 us: 26 ns a matrix instruction with random codes, 17.6 with zeros, as the
 // clock gives way to the power the products take.
 template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ? 1 : 2) void gemm_scaled_tile_kernel(ScaledGemm p)
 {
@@ -156,8 +158,10 @@ template <class T, int F, int STAGES> __global__ __launch_bounds__(256, F == 4 ?
         const auto leave = [&](int i, const T (&y)[V]) {
             const int m = mw + 32 * b + lane / LANES + i;
             T *const to = static_cast<T *>(p.Y) + m * p.ldy + n;
-            if (m < p.M && n + V <= p.N) __builtin_memcpy(to, y, sizeof y);          // (wherever a row begins)
-            else if (m < p.M)
+            if (m < p.M && n + V <= p.N) {
+                if (p.stream) __builtin_nontemporal_store(__builtin_bit_cast(i32x4_t, y), reinterpret_cast<i32x4_t *>(to));
+                else __builtin_memcpy(to, y, sizeof y);   // (wherever a row begins)
+            } else if (m < p.M)
 #pragma unroll
                 for (int j = 0; j < V - 1; ++j)
                     if (n + j < p.N) to[j] = y[j];
@@ -344,6 +348,7 @@ extern "C" int apnn_gemm_scaled(const int8_t *X_dev, const float *x_scale_dev, c
     if (!aligned_to(Y_dev, type)) return fail(APNN_ERR_ALIGNMENT, "apnn_gemm_scaled: Y is not aligned to its type");
     if (M > (1 << 26) || N > (1 << 26) || M * N > (int64_t(1) << 35) || ldy > INT64_MAX / 8 / M)
         return fail(APNN_ERR_UNSUPPORTED, "apnn_gemm_scaled: M = %lld, N = %lld, ldy = %lld", (long long)M, (long long)N, (long long)ldy);
-    const ScaledGemm p = {X_dev, W_dev, x_scale_dev, w_scale_dev, bias_dev, Y_dev, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(apnn_token_pitch(K)), 0, 0};
+    const ScaledGemm p = {X_dev, W_dev, x_scale_dev, w_scale_dev, bias_dev, Y_dev, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(apnn_token_pitch(K)), 0, 0,
+                          M * N * size_of(type) >= (16 << 20) && aligned16(Y_dev) && ldy * size_of(type) % 16 == 0};
     return by_type(type, [&](auto t) { return launch_scaled<decltype(t)>(p, as_stream(stream)); });
 }

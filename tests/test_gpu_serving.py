@@ -145,10 +145,10 @@ def test_gemm_scaled_in_every_form(M, N, K, form):
 
 
 def test_gemm_scaled_large():
-    """Sizes that choose the widest tiles by themselves, whole rounds of them and a part of one."""
-    for M, N, K in ((4096, 4096, 320), (4000, 4100, 144)):
+    """Sizes that choose the widest tiles by themselves, whole rounds of them and a part of one; results of 16 MiB and more."""
+    for M, N, K, dtype in ((4096, 4096, 320, BF16), (4000, 4100, 144, BF16), (2100, 2104, 64, F32), (8200, 1032, 48, F16)):
         X, xs, W, ws, bias = operands(M, N, K)
-        check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=bias, dtype=BF16), X, xs, W, ws, bias, BF16)
+        check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=bias, dtype=dtype), X, xs, W, ws, bias, dtype)
 
 
 def test_gemm_scaled_at_the_edge_of_int32():
