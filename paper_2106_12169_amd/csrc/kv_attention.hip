@@ -402,7 +402,7 @@ template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<
 //
 // Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (two where
 // D = 256) overlap: 34 % and 39 % of the cycles with two blocks of two tiles each, 245 us for prompts of up to 2048 tokens on
-// contexts of up to 4096, 32 heads on 8 of D = 128; 223 us (840 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
+// contexts of up to 4096, 32 heads on 8 of D = 128; 215 to 219 us (860 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
 // all rows, those of the next tile on their way meanwhile.  As for 16 rows, scores are computed transposed and the weights stay
 // in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
 // values are read in that order.
