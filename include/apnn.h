@@ -378,7 +378,8 @@ typedef struct {
 /* out = sum_t softmax_t(scale * q . k_t) v_t for every query head.  Query i of the n of a
  * sequence of l tokens stands at position l - n + i and sees the tokens at positions 0 up
  * to its own; one that sees none (l < n, l = 0) gets zeros.  Scores, softmax and sums are
- * held in fp32; the softmax's weights meet the values rounded to fp16, 11 bits.
+ * held in fp32; the softmax's weights meet the values rounded to fp16: by 2^-11 of a
+ * weight, or 2^-32 of the largest one where that is more.
  * Unseen tokens count for nothing whatever their keys and values hold; one that holds NaN
  * and is seen makes the query's result NaN.
  * Rows of out that no sequence has are left as they were, and so are queries beyond

@@ -1,0 +1,49 @@
+"""Attention over the 4-bit cache where scores, weights and cached bytes are unusual, against closed forms and 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as O
+from paper_2106_12169_amd import binding as B
+from tests.test_gpu_serving import BF16, F16, F32, close, dense, f64, filled, normal, rng, rows  # noqa: F401  (rows: a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(values, dtype=torch.int32):
+    return torch.tensor(values, dtype=dtype, device="cuda")
+
+
+def sink_and_tail(l, heads, D, page, at):
+    """A sequence whose token `at` has key 1 and value 0, all the others key 0 and value 1: every number of it is one of the cache."""
+    pages = -(-l // page)
+    cache = B.KVCache.empty(pages, heads, page, D)
+    k, v = torch.zeros((l, heads, D), device="cuda"), torch.ones((l, heads, D), device="cuda")
+    k[at], v[at] = 1.0, 0.0
+    B.apnn_kv_append(cache, k, v, torch.arange(l, device="cuda"))
+    return cache, torch.arange(pages, dtype=torch.int32, device="cuda").reshape(1, -1)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("l, D, at", [(20000, 64, 0), (20000, 128, 7777), (700, 96, 0), (3000, 256, 2999), (131072, 128, 0)])
+def test_a_long_tail_of_small_weights(l, D, at, dtype, rows):
+    """One token of value 0 with the largest weight and a tail e^-gap below it: the result is the tail's share.
+
+    Scores are exact: products of 1 with 0 or 1.  In powers of two the gap is 1.4427 gap, off by at most 3 2^-24 of it (constant, scale,
+    product), and v_exp_f32 adds 2^-22, to a tail weight w: 2^-21 w (1 + gap).  A weight is rounded by 2^-11 of it, or by 2^-32 of the largest
+    one; sums of l terms of one sign are off by l 2^-24 of themselves at most, in any order.  Both count in the numerator and in the sum."""
+    cache, pages = sink_and_tail(l, 2, D, 64, at)
+    news = 70 if D == 64 else 3
+    q = torch.ones((news, 4, D), dtype=dtype, device="cuda")
+    for gap in (6.0, 10.0, 14.0, 16.0, 17.0, 17.5, 18.0):
+        scale = float(np.float32(gap / D))
+        out = B.apnn_kv_attention(cache, q, ints([l]), pages, scale, q_start=ints([0, news]), max_q=news)
+        w = np.exp(-scale * D)
+        for i in range(news):
+            tail = l - news + i                           # tokens seen beside the sink
+            if l - news + i < at:                         # (the sink is not seen yet: all weights are equal)
+                want = 1.0
+            else:
+                want = tail * w / (1 + tail * w)
+            rel = 2.0 ** -11 + 2 * (2.0 ** -21 * (1 + gap) + l * 2.0 ** -24)
+            close(out[i], np.full((4, D), want), dtype, rel * want + l * 2.0 ** -32)
