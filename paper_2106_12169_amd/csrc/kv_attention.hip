@@ -113,6 +113,22 @@ __device__ __forceinline__ float column_max(float x)
     return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
+// Two queries times the scale's sign, -1, 0 or 1: exact, and 0 makes NaN of what is not finite.  The scores' factor is then positive, in powers of
+// two: with 0 there, an unseen token's -inf would become NaN.
+template <class T> __device__ __forceinline__ uint32_t times_sign(uint32_t w, float sign);
+template <> __device__ __forceinline__ uint32_t times_sign<_Float16>(uint32_t w, float sign)
+{
+    const _Float16 s = static_cast<_Float16>(sign);
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, w) * half2_t{s, s});
+}
+template <> __device__ __forceinline__ uint32_t times_sign<__bf16>(uint32_t w, float sign)
+{
+    const bf16x2_t x = __builtin_bit_cast(bf16x2_t, w);
+    return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(static_cast<float>(x[0]) * sign), static_cast<__bf16>(static_cast<float>(x[1]) * sign)});
+}
+__device__ __forceinline__ float sign_of(float scale) { return scale == 0.0f ? 0.0f : copysignf(1.0f, scale); }
+__device__ __forceinline__ float factor_of(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale) * 1.4426950408889634f; }
+
 // What a block works on: 16 or 128 rows (queries x the heads that share a cache head, heads inside) of one sequence and cache head.
 struct Rows {
     int64_t q0;                                           // first query row of the sequence
@@ -228,15 +244,17 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     {
         const int qh = head * a.group + (live ? r - i * a.group : 0);
         const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + quarter * (D / 4);
-        const uint32_t flip = a.d.scale < 0.0f ? 0x80008000u : 0u;       // a negative scale is the queries'
+        const float sign = sign_of(a.d.scale);
 #pragma unroll
         for (int s = 0; s < steps; ++s) {
             u32x4_t w;
             __builtin_memcpy(&w, src + 8 * s, 16);        // (however they are aligned)
-            q[s] = __builtin_bit_cast(typename Op::vec, w ^ flip);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = times_sign<T>(w[j], sign);
+            q[s] = __builtin_bit_cast(typename Op::vec, w);
         }
     }
-    const float factor = fabsf(a.d.scale) * 1.4426950408889634f;         // scores in powers of two
+    const float factor = factor_of(a.d.scale);
     const PageTable pages = table_of(a, b);
     char *const mine = lds[wave];
     const int token = lane >> 2, piece = lane & 3;        // as loaded
@@ -443,15 +461,17 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     {
         const int qh = head * a.group + (live ? r - i * a.group : 0);
         const T *src = static_cast<const T *>(a.d.q_dev) + (x.q0 + (live ? i : 0)) * a.d.q_token_stride + qh * a.d.q_head_stride + 8 * half;
-        const uint32_t flip = a.d.scale < 0.0f ? 0x80008000u : 0u;       // a negative scale is the queries'
+        const float sign = sign_of(a.d.scale);
 #pragma unroll
         for (int s = 0; s < steps; ++s) {
             u32x4_t w;
             __builtin_memcpy(&w, src + 16 * s, 16);
-            q[s] = __builtin_bit_cast(typename Op::vec, w ^ flip);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = times_sign<T>(w[j], sign);
+            q[s] = __builtin_bit_cast(typename Op::vec, w);
         }
     }
-    const float factor = fabsf(a.d.scale) * 1.4426950408889634f;         // scores in powers of two
+    const float factor = factor_of(a.d.scale);
     const int32_t *pages = a.d.page_dev + place.seq * a.d.max_pages;
     const int mask = (1 << a.page_shift) - 1;
 
@@ -778,7 +798,6 @@ extern "C" int apnn_kv_attention(const apnn_kv_attention_desc *desc, const apnn_
     a.c = *cache;
     a.d.max_q = plan.max_q;
     if (cache->pages == 0) a.d.max_pages = 0;             // no page can be read
-    if (desc->scale == 0.0f) a.d.scale = 1e-37f;          // every weight 1 (no score reaches 2^40), and -inf, an unseen token, stays what it is
     a.parts = static_cast<float *>(workspace_dev);
     a.tiles = plan.tiles;
     a.page_shift = shift_of(cache->page_size);

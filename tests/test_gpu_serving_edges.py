@@ -47,3 +47,25 @@ def test_a_long_tail_of_small_weights(l, D, at, dtype, rows):
                 want = tail * w / (1 + tail * w)
             rel = 2.0 ** -11 + 2 * (2.0 ** -21 * (1 + gap) + l * 2.0 ** -24)
             close(out[i], np.full((4, D), want), dtype, rel * want + l * 2.0 ** -32)
+
+
+@pytest.mark.parametrize("news", [1, 40])
+def test_scale_zero_is_the_average_whatever_the_queries(news, rows):
+    """Finite queries of any size with scale 0: equal weights, so sums of values in fp32: l 2^-24 of the sum of magnitudes, twice."""
+    l, D = 200, 64
+    cache, table = filled(rng(50), [l], 2, 16, D)
+    k, v = dense(cache, table, 0, l)
+    for size in (1.0, 1e30, 3e38):
+        q = (normal(rng(51), news, 4, D).clamp(-1, 1) * size).to(BF16)
+        q[0, 1] = 0
+        out = B.apnn_kv_attention(cache, q, ints([l]), table, 0.0, q_start=ints([0, news]), max_q=news)
+        for i in range(news):
+            seen = l - news + i + 1
+            for h in range(4):
+                close(out[i, h], v[:seen, h // 2].mean(0), BF16, 2 * l * 2.0 ** -24 * np.abs(v[:seen, h // 2]).mean(0))
+    q[0, 2, 5], q[-1, 3, 0] = float("nan"), float("-inf")               # 0 times these is not 0
+    out = B.apnn_kv_attention(cache, q, ints([l]), table, 0.0, q_start=ints([0, news]), max_q=news)
+    want = np.zeros((news, 4), bool)
+    want[0, 2] = want[-1, 3] = True
+    np.testing.assert_array_equal(torch.isnan(out).all(-1).cpu().numpy(), want)
+    np.testing.assert_array_equal(torch.isnan(out).any(-1).cpu().numpy(), want)
