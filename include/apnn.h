@@ -380,6 +380,8 @@ typedef struct {
  * to its own; one that sees none (l < n, l = 0) gets zeros.  Scores, softmax and sums are
  * held in fp32; the softmax's weights meet the values rounded to fp16: by 2^-11 of a
  * weight, or 2^-32 of the largest one where that is more.
+ * A query that sees a token gets NaN if it is not finite, and if its scores exceed fp32's
+ * range, before the scale or after it, upwards or all of them downwards.
  * Unseen tokens count for nothing whatever their keys and values hold; one that holds NaN
  * and is seen makes the query's result NaN.
  * Rows of out that no sequence has are left as they were, and so are queries beyond

@@ -165,6 +165,18 @@ __device__ __forceinline__ Rows find_rows(const AttentionArgs &a, int64_t b, int
     return x;
 }
 
+// What 1 / (sum of weights) is for a query whose weights sum to 0: 0 if no token that it sees is in a page of the cache, NaN if all scores are -inf or
+// the maximum is beyond fp32 (infinite queries, sums and scales out of range).  The loops over tokens need not know; this is looked up at the end.
+__device__ __forceinline__ float inverse_of_nothing(const AttentionArgs &a, const Rows &x, int64_t seq, int i)
+{
+    const int seen = seen_by(x, i);
+    for (int p = 0; p << a.page_shift < seen; ++p) {
+        const int page = a.d.page_dev[seq * a.d.max_pages + p];
+        if (page >= 0 && page < a.c.pages) return __uint_as_float(0x7FC00000u);
+    }
+    return 0.0f;
+}
+
 // Tile, cache head and sequence of a block.  Heads and sequences change fastest: blocks go to the eight XCDs in turn, so that the
 // tiles of one head find its codes in the L2 of the same XCD as long as heads x seqs is a multiple of 8; the tiles that see the
 // most tokens come first.
@@ -405,7 +417,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                 part[D + 1] = l;
             }
         } else {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const float inv = l == 0.0f ? inverse_of_nothing(a, x, b, ri) : 1.0f / l;
             T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + ch;
             for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
         }
@@ -613,7 +625,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         }
         return;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = sum == 0.0f ? inverse_of_nothing(a, x, place.seq, i) : 1.0f / sum;
     T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + i) * a.d.out_token_stride + (head * a.group + (r - i * a.group)) * a.d.out_head_stride + 4 * half;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -692,7 +704,7 @@ template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_a
             l += weights[s] * f;
         }
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? inverse_of_nothing(a, x, place.seq, ri) : 1.0f / l;
     T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + 4 * lane;
     T y[4];
 #pragma unroll

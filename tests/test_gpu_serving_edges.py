@@ -69,3 +69,33 @@ def test_scale_zero_is_the_average_whatever_the_queries(news, rows):
     want[0, 2] = want[-1, 3] = True
     np.testing.assert_array_equal(torch.isnan(out).all(-1).cpu().numpy(), want)
     np.testing.assert_array_equal(torch.isnan(out).any(-1).cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("l", [1, 40, 3000])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_queries_and_scores_beyond_range_give_nan(l, dtype, rows):
+    """No number is the softmax of scores that are infinite or leave fp32's range, upwards or downwards; others in the batch are not touched,
+    and a query that sees nothing still gets zeros."""
+    D, H = 64, 2
+    pages = -(-l // 64) + 1
+    cache = B.KVCache.empty(pages, H, 64, D)
+    k = torch.ones((l, H, D), device="cuda")
+    B.apnn_kv_append(cache, k, k, torch.arange(l, device="cuda"))
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").reshape(1, -1)
+    news = 3
+    q = torch.ones((news, H, D), dtype=dtype, device="cuda")
+    q[2, 0, 5], q[1, 1, 63] = float("-inf"), float("inf")
+    out = B.apnn_kv_attention(cache, q, ints([l]), table, 0.125, q_start=ints([0, news]), max_q=news)
+    want = torch.ones((news, H), device="cuda")
+    want[2, 0] = want[1, 1] = float("nan")
+    for i in range(news):
+        if l - news + i + 1 <= 0:
+            want[i] = 0
+    assert torch.equal(torch.nan_to_num(out.float(), nan=7.0), torch.nan_to_num(want, nan=7.0)[:, :, None].expand(news, H, D))
+    nothing = torch.full_like(table, -1)
+    assert (B.apnn_kv_attention(cache, q, ints([l]), nothing, 0.125, q_start=ints([0, news]), max_q=news) == 0).all()
+    q = torch.ones((1, H, D), dtype=dtype, device="cuda")
+    for scale in (1e37, -1e37):                           # 64 of it is beyond fp32
+        assert torch.isnan(B.apnn_kv_attention(cache, q, ints([l]), table, scale)).all()
+    assert torch.equal(B.apnn_kv_attention(cache, q, ints([l]), table, 1e35), q)
+    assert torch.equal(B.apnn_kv_attention(cache, q, ints([l]), table, -1e35), q)
