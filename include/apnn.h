@@ -382,8 +382,9 @@ typedef struct {
  * weight, or 2^-32 of the largest one where that is more.
  * A query that sees a token gets NaN if it is not finite, and if its scores exceed fp32's
  * range, before the scale or after it, upwards or all of them downwards.
- * Unseen tokens count for nothing whatever their keys and values hold; one that holds NaN
- * and is seen makes the query's result NaN.
+ * Unseen tokens count for nothing whatever bytes their keys and values hold; one that holds
+ * NaN and is seen makes the query's result NaN.  (Value scale bytes above 140, which are
+ * none of the format's, are taken as 140.)
  * Rows of out that no sequence has are left as they were, and so are queries beyond
  * max_q.  Tokens beyond the table's max_pages, and tokens of pages outside the cache, are
  * never read and count as unseen.

@@ -60,6 +60,8 @@ template <class T> __device__ __forceinline__ u32x4_t values8(uint32_t w, float 
 
 // A row's scale as the conversions take it; 255 stands for NaN there too.
 __device__ __forceinline__ float unit_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// Values': no more than the largest power of two that a value has, whatever the byte, so that the weight 0 of an unseen token leaves nothing of it.
+__device__ __forceinline__ float value_unit_of(uint32_t byte) { return unit_of(min(byte, 140u)); }
 
 // A quarter's share of a row: channels [D / 4 * quarter, + D / 4).  In a matrix instruction lane l has quarter l / 16 of token
 // l % 16; loaded neighbours lie side by side in the cache, lane l with quarter l % 4 of token l / 4.
@@ -127,7 +129,11 @@ template <> __device__ __forceinline__ uint32_t times_sign<__bf16>(uint32_t w, f
     return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(static_cast<float>(x[0]) * sign), static_cast<__bf16>(static_cast<float>(x[1]) * sign)});
 }
 __device__ __forceinline__ float sign_of(float scale) { return scale == 0.0f ? 0.0f : copysignf(1.0f, scale); }
-__device__ __forceinline__ float factor_of(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale) * 1.4426950408889634f; }
+__device__ __forceinline__ float factor_of(float scale)
+{
+    const float f = scale == 0.0f ? 1.0f : fabsf(scale) * 1.4426950408889634f;
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f)));        // (one for the wave: a scalar register)
+}
 
 // What a block works on: 16 or 128 rows (queries x the heads that share a cache head, heads inside) of one sequence and cache head.
 struct Rows {
@@ -251,7 +257,8 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
 
     const int r = x.r0 + c, i = r / a.group;
     const bool live = i < x.n;
-    const int seen = live ? seen_by(x, i) : 0, least = seen_by(x, x.r0 / a.group);       // (all rows see the tokens before `least`)
+    // tokens that the row sees, from the first that a lane has scores of on; all rows see the tokens before `least`
+    const int seen = (live ? seen_by(x, i) : 0) - 4 * quarter, least = seen_by(x, x.r0 / a.group);
     typename Op::vec q[steps];
     {
         const int qh = head * a.group + (live ? r - i * a.group : 0);
@@ -307,11 +314,10 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         f32x4_t score[2] = {};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bool written = now.there[u] && t0 + 16 * u + token < x.have;     // beyond the end: whatever it is, made finite
 #pragma unroll
             for (int s = 0; s < steps; ++s) {
                 const bool second = Share<D>::units > 1 && Share<D>::unit(piece, s);
-                const u32x4_t v = values8<_Float16>(now.v[u].w[s], unit_of(written ? now.vu[u][second ? Share<D>::units - 1 : 0] : 127));
+                const u32x4_t v = values8<_Float16>(now.v[u].w[s], value_unit_of(now.vu[u][second ? Share<D>::units - 1 : 0]));
                 *reinterpret_cast<u32x4_t *>(mine + (16 * u + token) * kValueRow<D> + (piece * (D / 4) + 8 * s) * 2) = v;
             }
 #pragma unroll
@@ -324,7 +330,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         if (t0 + tokens > least || !now.there[0] || !now.there[1]) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int limit = now.there[u] ? seen - t0 - 16 * u - 4 * quarter : 0;
+                const int limit = now.there[u] ? seen - t0 - 16 * u : 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) score[u][j] = j < limit ? score[u][j] : -INFINITY;
             }
@@ -489,13 +495,12 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
 
     // loader: thread 4 t + u has token t of a tile and channels [D / 4 u, + D / 4)
     const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
-    struct Row { Codes<D> k, v; uint8_t ku[Share<D>::units], vu[Share<D>::units]; bool there, written; };
+    struct Row { Codes<D> k, v; uint8_t ku[Share<D>::units], vu[Share<D>::units]; bool there; };
     const auto page_of = [&](int t0) { return t0 + token < end ? pages[(t0 + token) >> a.page_shift] : -1; };
     const auto fetch = [&](int t0, int page) {
         Row f;
         const int t = t0 + token;
         f.there = t < end && page >= 0 && page < a.c.pages;
-        f.written = f.there && t < x.have;
         const int64_t row = ((static_cast<int64_t>(f.there ? page : 0) * a.c.heads + head) << a.page_shift) + (t & mask);
         const int64_t code_at = row * (D / 2) + quarter * (D / 8), unit_at = row * (D / 32) + quarter * (D / 4) / 32;
         f.k = *reinterpret_cast<const Codes<D> *>(a.c.k_codes_dev + code_at);
@@ -515,7 +520,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         for (int s = 0; s < words; ++s) {
             const bool second = Share<D>::units > 1 && Share<D>::unit(quarter, s);
             *reinterpret_cast<u32x4_t *>(k_to + 16 * s) = values8<T>(f.k.w[s], unit_of(f.ku[second ? Share<D>::units - 1 : 0]));
-            *reinterpret_cast<u32x4_t *>(v_to + 16 * s) = values8<_Float16>(f.v.w[s], unit_of(f.written ? f.vu[second ? Share<D>::units - 1 : 0] : 127));
+            *reinterpret_cast<u32x4_t *>(v_to + 16 * s) = values8<_Float16>(f.v.w[s], value_unit_of(f.vu[second ? Share<D>::units - 1 : 0]));
         }
         if ((threadIdx.x & 63) == 0) pages_there[token / 16] = f.there;
     };

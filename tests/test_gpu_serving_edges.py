@@ -99,3 +99,22 @@ def test_queries_and_scores_beyond_range_give_nan(l, dtype, rows):
         assert torch.isnan(B.apnn_kv_attention(cache, q, ints([l]), table, scale)).all()
     assert torch.equal(B.apnn_kv_attention(cache, q, ints([l]), table, 1e35), q)
     assert torch.equal(B.apnn_kv_attention(cache, q, ints([l]), table, -1e35), q)
+
+
+@pytest.mark.parametrize("l, news", [(300, 40), (300, 200), (3000, 4)])
+def test_values_of_unseen_tokens_may_be_any_bytes(l, news, rows):
+    """Value scale bytes that append never writes, in tokens that stand after the query: nothing of them reaches it."""
+    D, page = 64, 16
+    g = rng(60 + news)
+    cache, table = filled(g, [l], 2, page, D)
+    q = normal(g, news, 4, D, dtype=F16)
+    run = lambda: B.apnn_kv_attention(cache, q, ints([l]), table, 0.125, q_start=ints([0, news]), max_q=news)  # noqa: E731
+    good = run()
+    first = l - news // 2                                 # tokens from here on: seen by the later queries only
+    for t in range(first, l):
+        at = int(table[0, t // page])
+        cache.v_scale[at, :, t % page] = 255 if t % 2 else 150
+    some = news - (l - first)                             # queries that see none of them
+    assert some > 0
+    got = run()
+    assert torch.equal(got[:some], good[:some])
