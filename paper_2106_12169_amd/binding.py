@@ -363,6 +363,9 @@ def apnn_sumpool_fc(X: torch.Tensor, N: int, H: int, W: int, Cc: int, bits: int,
     return out
 
 
+# The operators below are for inference: they refuse tensors that require gradients unless called under torch.no_grad() (or inference_mode), and
+# their results have none.
+
 def apnn_token_pitch(K: int) -> int:
     """Bytes of a row of 8-bit codes: K rounded up to 16."""
     return lib().apnn_token_pitch(K)

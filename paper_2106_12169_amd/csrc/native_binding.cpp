@@ -9,6 +9,7 @@
 //
 // As with ctypes, the interpreter lock is released while the library runs (a launch can wait for queue space).
 #include <Python.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
@@ -378,7 +379,7 @@ PyObject *py_sumpool_fc(PyObject *, PyObject *const *args, Py_ssize_t n)    // (
 
 // ---- operators on typed tensors (8-bit products with scales, the 4-bit cache): their sizes, types and strides are the tensors'
 // own, so they are checked here; what the library checks itself is left to it.  All tensors of a call lie on one device, whose
-// current stream is used whichever device is current.
+// current stream is used whichever device is current.  There is no backward pass: what autograd would have to follow is refused.
 
 class Tensors {
 public:
@@ -398,6 +399,8 @@ public:
         if (!THPVariable_Check(o)) return fail(PyExc_TypeError, "%s: a torch tensor is expected", name);
         const at::Tensor &t = THPVariable_Unpack(o);
         if (!t.is_cuda()) return fail(PyExc_AssertionError, "%s: a device tensor is expected", name);
+        if (t.requires_grad() && at::GradMode::is_enabled())
+            return fail(PyExc_RuntimeError, "%s: requires a gradient, and there is no backward pass (detach it, or call under torch.no_grad())", name);
         if (dim >= 0 && t.dim() != dim) return fail(PyExc_ValueError, "%s: %d dimensions are expected, got %lld", name, dim, static_cast<long long>(t.dim()));
         if (t.dim() && t.size(-1) > 1 && t.stride(-1) != 1) return fail(PyExc_AssertionError, "%s: the last dimension has to be contiguous", name);
         for (int64_t s : t.strides())

@@ -118,3 +118,24 @@ def test_values_of_unseen_tokens_may_be_any_bytes(l, news, rows):
     assert some > 0
     got = run()
     assert torch.equal(got[:some], good[:some])
+
+
+def test_inputs_that_require_gradients_are_refused():
+    x = torch.randn(4, 32, device="cuda", requires_grad=True)
+    with pytest.raises(RuntimeError, match="src: .*gradient"):
+        B.apnn_quantize_tokens(x)
+    with torch.no_grad():
+        codes, scale = B.apnn_quantize_tokens(x)
+    bias = torch.randn(4, device="cuda", requires_grad=True)
+    with pytest.raises(RuntimeError, match="bias: .*gradient"):
+        B.apnn_gemm_scaled(codes, scale, codes, scale, 32, bias=bias)
+    assert not B.apnn_gemm_scaled(codes, scale, codes, scale, 32, bias=bias.detach()).requires_grad
+    cache = B.KVCache.empty(1, 1, 16, 64)
+    k = torch.randn(2, 1, 64, device="cuda")
+    q = torch.randn(2, 1, 64, device="cuda", dtype=F16, requires_grad=True)
+    with pytest.raises(RuntimeError, match="k: .*gradient"):
+        B.apnn_kv_append(cache, k.requires_grad_(), k, torch.arange(2, device="cuda"))
+    with pytest.raises(RuntimeError, match="q: .*gradient"):
+        B.apnn_kv_attention(cache, q, ints([1, 2]), ints([[0], [0]]), 1.0)
+    with torch.inference_mode():
+        B.apnn_kv_attention(cache, q, ints([1, 2]), ints([[0], [0]]), 1.0, out=torch.empty_like(q))
