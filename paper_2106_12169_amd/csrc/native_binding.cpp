@@ -13,6 +13,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <c10/util/SmallVector.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -379,7 +380,8 @@ PyObject *py_sumpool_fc(PyObject *, PyObject *const *args, Py_ssize_t n)    // (
 
 // ---- operators on typed tensors (8-bit products with scales, the 4-bit cache): their sizes, types and strides are the tensors'
 // own, so they are checked here; what the library checks itself is left to it.  All tensors of a call lie on one device, whose
-// current stream is used whichever device is current.  There is no backward pass: what autograd would have to follow is refused.
+// current stream is used whichever device is current.  There is no backward pass: what autograd would have to follow is refused, and what
+// a call writes into counts as changed, so that a backward pass that needs its old values fails.
 
 class Tensors {
 public:
@@ -480,7 +482,13 @@ public:
         if (t->scalar_type() != type) fail(PyExc_TypeError, "%s: type %s is expected, got %s", name, c10::toString(type), c10::toString(t->scalar_type()));
         if (ok_ && dense && !t->is_contiguous()) fail(PyExc_AssertionError, "%s: a contiguous tensor is expected", name);
         sizes(name, t, want);
+        if (ok_) writes(t);
         return *t;
+    }
+    // The call writes into this tensor of the caller's.
+    void writes(const at::Tensor *t)
+    {
+        if (!t->is_inference()) written_.push_back(t->unsafeGetTensorImpl());
     }
     // Whether the next argument is None; it is passed over if so.
     bool none()
@@ -499,6 +507,8 @@ public:
         Py_BEGIN_ALLOW_THREADS
         rc = f(stream);
         Py_END_ALLOW_THREADS
+        if (rc == APNN_OK)
+            for (c10::TensorImpl *t : written_) t->bump_version();
         return finish(rc);
     }
 
@@ -514,6 +524,7 @@ private:
     Py_ssize_t i_ = 0;
     bool ok_ = true, have_device_ = false;
     at::Device device_ = at::Device(at::kCUDA, 0);
+    c10::SmallVector<c10::TensorImpl *, 4> written_;
 };
 
 template <class T> T *data(const at::Tensor *t) { return t ? static_cast<T *>(t->data_ptr()) : nullptr; }
@@ -576,6 +587,7 @@ PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)
     } else if (const at::Tensor *given = a.strided("out", 2)) {
         out = *given;
         a.sizes("out", given, {M, N});
+        a.writes(given);
     }
     const apnn_dtype type = a.type("out", &out);
     if (!a.ok()) return nullptr;
@@ -585,8 +597,8 @@ PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)
     }), out);
 }
 
-// the four arrays of a binding.KVCache
-apnn_kv_cache read_cache(Tensors &a)
+// the four arrays of a binding.KVCache, which the call may write into
+apnn_kv_cache read_cache(Tensors &a, bool written = false)
 {
     apnn_kv_cache c = {};
     const at::Tensor *kc = a.dense("k_codes", 4, at::kByte), *ks = a.dense("k_scale", 4, at::kByte), *vc = a.dense("v_codes", 4, at::kByte), *vs = a.dense("v_scale", 4, at::kByte);
@@ -596,6 +608,8 @@ apnn_kv_cache read_cache(Tensors &a)
     a.sizes("v_codes", vc, {pages, heads, page, D / 2});
     a.sizes("v_scale", vs, {pages, heads, page, D / 32});
     if (!a.ok()) return c;
+    if (written)
+        for (const at::Tensor *t : {kc, ks, vc, vs}) a.writes(t);
     c.k_codes_dev = data<uint8_t>(kc);
     c.k_scale_dev = data<uint8_t>(ks);
     c.v_codes_dev = data<uint8_t>(vc);
@@ -612,7 +626,7 @@ apnn_kv_cache read_cache(Tensors &a)
 PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     Tensors a(args, n, 12);
-    const apnn_kv_cache c = read_cache(a);
+    const apnn_kv_cache c = read_cache(a, true);
     const at::Tensor *k = a.strided("k", 3), *v = a.strided("v", 3), *slots = a.dense("slots", 1, at::kLong);
     const at::Tensor *positions = a.dense("positions", 1, at::kInt, true), *table = a.dense("table", 2, at::kFloat, true);
     const long long interleaved = a.integer();

@@ -139,3 +139,18 @@ def test_inputs_that_require_gradients_are_refused():
         B.apnn_kv_attention(cache, q, ints([1, 2]), ints([[0], [0]]), 1.0)
     with torch.inference_mode():
         B.apnn_kv_attention(cache, q, ints([1, 2]), ints([[0], [0]]), 1.0, out=torch.empty_like(q))
+
+
+def test_results_written_in_place_are_seen_by_autograd():
+    """A tensor that a backward pass needs and a call has overwritten makes that pass fail instead of using the new values."""
+    cache, w = B.KVCache.empty(1, 1, 16, 64), torch.randn(64, device="cuda", requires_grad=True)
+    q, k = torch.randn(2, 1, 64, device="cuda"), torch.randn(2, 1, 64, device="cuda")
+    y = (q * w).sum()
+    table = torch.ones((4, 64), device="cuda")
+    B.apnn_kv_append(cache, k, k, torch.arange(2, device="cuda"), q=q, q_out=q, table=table, positions=ints([1, 2]))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    out = torch.empty((2, 1, 64), device="cuda", dtype=F16)
+    before = out._version
+    B.apnn_kv_attention(cache, q.half(), ints([1, 2]), ints([[0], [0]]), 1.0, out=out)
+    assert out._version == before + 1
