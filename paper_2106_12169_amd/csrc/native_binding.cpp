@@ -17,6 +17,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstring>
 #include <exception>
 #include <new>
@@ -597,6 +598,9 @@ PyObject *py_gemm_scaled(PyObject *, PyObject *const *args, Py_ssize_t n)
     }), out);
 }
 
+// A size that the library takes as 32 bits; what does not fit is one that it refuses.
+int narrow(int64_t v) { return static_cast<int>(std::clamp<int64_t>(v, INT32_MIN, INT32_MAX)); }
+
 // the four arrays of a binding.KVCache, which the call may write into
 apnn_kv_cache read_cache(Tensors &a, bool written = false)
 {
@@ -615,7 +619,6 @@ apnn_kv_cache read_cache(Tensors &a, bool written = false)
     c.v_codes_dev = data<uint8_t>(vc);
     c.v_scale_dev = data<uint8_t>(vs);
     c.pages = pages;
-    const auto narrow = [](int64_t v) { return static_cast<int>(v > INT32_MAX ? INT32_MAX : v); };      // (refused by the library either way)
     c.heads = narrow(heads);
     c.page_size = narrow(page);
     c.D = narrow(D);
@@ -656,14 +659,14 @@ PyObject *py_kv_append(PyObject *, PyObject *const *args, Py_ssize_t n)
     t.v_token_stride = v->stride(0); t.v_head_stride = v->stride(1);
     t.slot_dev = data<int64_t>(slots);
     if (table) {
-        t.rot = static_cast<int>(table->size(1) > INT32_MAX ? INT32_MAX : table->size(1));
+        t.rot = narrow(table->size(1));
         t.interleaved = interleaved != 0;
         t.table_dev = data<float>(table);
         t.table_rows = table->size(0);
         t.position_dev = data<int32_t>(positions);
     }
     if (q && q->size(1)) {
-        t.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
+        t.q_heads = narrow(q->size(1));
         t.q_dev = data<void>(q);
         t.q_out_dev = data<void>(&q_out);
         t.q_token_stride = q->stride(0); t.q_head_stride = q->stride(1);
@@ -710,7 +713,7 @@ PyObject *py_kv_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
     a.sizes("q_start", q_start, {d.seqs + 1});
     const at::Tensor out = a.result("out", {d.tokens, q->size(1), c.D}, q->scalar_type(), false), *workspace = a.dense("workspace", 1, at::kByte, true);
     if (!a.ok()) return nullptr;
-    d.q_heads = static_cast<int>(q->size(1) > INT32_MAX ? INT32_MAX : q->size(1));
+    d.q_heads = narrow(q->size(1));
     d.q_dev = data<void>(q);
     d.out_dev = data<void>(&out);
     d.q_token_stride = q->stride(0); d.q_head_stride = q->stride(1);
@@ -736,11 +739,11 @@ PyObject *py_kv_attention_workspace(PyObject *, PyObject *const *args, Py_ssize_
     Tensors a(args, n, 9);
     apnn_kv_cache c = {};
     apnn_kv_attention_desc d = {};
-    c.heads = static_cast<int>(a.integer());
-    c.page_size = static_cast<int>(a.integer());
-    c.D = static_cast<int>(a.integer());
+    c.heads = narrow(a.integer());
+    c.page_size = narrow(a.integer());
+    c.D = narrow(a.integer());
     d.tokens = a.integer();
-    d.q_heads = static_cast<int>(a.integer());
+    d.q_heads = narrow(a.integer());
     d.seqs = a.integer();
     d.max_pages = a.integer();
     static const int32_t some = 0;

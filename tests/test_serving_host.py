@@ -155,3 +155,15 @@ def test_the_binding_refuses_what_is_no_device_tensor():
         B.apnn_kv_read(c, torch.zeros(1, dtype=torch.int64))
     with pytest.raises(B.ApnnError, match="pages of 24 tokens"):
         B.native().kv_attention_workspace(1, 24, 64, 1, 1, 1, 1, False, 1)
+
+
+@pytest.mark.parametrize("at", [0, 1, 2, 4])
+def test_sizes_beyond_32_bits_are_refused_and_not_cut_off(at):
+    """heads, page size, channels and query heads of the workspace's size; 2^32 more than a size that is right, or less."""
+    good = [2, 16, 64, 1, 4, 1, 4096, False, 1]
+    assert B.native().kv_attention_workspace(*good) > 0
+    for far in (1 << 32, -(1 << 32), 1 << 62):
+        bad = list(good)
+        bad[at] += far
+        with pytest.raises(B.ApnnError):
+            B.native().kv_attention_workspace(*bad)
