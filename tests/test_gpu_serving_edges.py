@@ -1,11 +1,11 @@
-"""Attention over the 4-bit cache where scores, weights and cached bytes are unusual, against closed forms and 64 bits."""
+"""The operators of low-bit language models where sizes, scores, weights and cached bytes are unusual, against closed forms and 64 bits."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import serving as O
 from paper_2106_12169_amd import binding as B
-from tests.test_gpu_serving import BF16, F16, F32, close, dense, f64, filled, normal, rng, rows  # noqa: F401  (rows: a fixture)
+from tests.test_gpu_serving import BF16, F16, F32, attend, check_product, close, dense, f64, filled, normal, operands, rng, rows  # noqa: F401  (rows: a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -118,6 +118,25 @@ def test_values_of_unseen_tokens_may_be_any_bytes(l, news, rows):
     assert some > 0
     got = run()
     assert torch.equal(got[:some], good[:some])
+
+
+# two, three and four tiles of channels a block with as many of tokens, sizes that end inside a tile
+WIDE = [(20, 6150, 200), (40, 9300, 333), (17, 12301, 129), (48, 6200, 64), (33, 6145, 1000), (45, 12300, 130), (64, 6161, 100), (60, 9217, 65), (50, 12305, 47),
+        (31, 9999, 77), (100, 2601, 77), (128, 5200, 300), (128, 7700, 300), (66, 5121, 500), (127, 10240, 33)]
+
+
+@pytest.mark.parametrize("M, N, K", WIDE)
+def test_few_tokens_against_wide_layers(M, N, K):
+    """The forms that read the tokens less often, which need many channels; and nothing is written beside a strided result."""
+    X, xs, W, ws, bias = operands(M, N, K, low=-128)
+    for dtype, b in ((F32, bias), (F16, None), (BF16, bias)):
+        check_product(B.apnn_gemm_scaled(X, xs, W, ws, K, bias=b, dtype=dtype), X, xs, W, ws, b, dtype)
+    whole = torch.full((M + 2, N + 5), 7.0, dtype=BF16, device="cuda")
+    out = whole[1:M + 1, 3:N + 3]
+    B.apnn_gemm_scaled(X, xs, W, ws, K, bias=bias, out=out)
+    check_product(out, X, xs, W, ws, bias, BF16)
+    out.fill_(7.0)
+    assert (whole == 7.0).all()
 
 
 def test_inputs_that_require_gradients_are_refused():
