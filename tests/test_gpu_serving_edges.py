@@ -120,6 +120,54 @@ def test_values_of_unseen_tokens_may_be_any_bytes(l, news, rows):
     assert torch.equal(got[:some], good[:some])
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D, Hq, heads", [(96, 6, 2), (256, 4, 1), (64, 3, 3), (128, 8, 2)])
+def test_long_contexts_of_every_size_of_head(D, Hq, heads, dtype, rows):
+    """Parts of splits joined by both kernels that join, for every number of channels."""
+    attend(100 + D, [9000, 1100, 5000], [1, 1, 1], Hq, heads, D, 64, dtype)        # up to 36 parts: a block to a row
+    attend(200 + D, [6000, 1300], [40, 7], Hq, heads, D, 32, dtype)
+    attend(300 + D, [2100] * 12, [1] * 12, 8 * (Hq // heads), 8, D, 16, dtype)      # 96 blocks, 5 parts: a team of lanes to a row
+
+
+@pytest.mark.parametrize("D, heads", [(64, 2), (128, 4), (256, 1)])
+def test_parts_beyond_one_pass_of_the_join(D, heads):
+    """131072 tokens: more parts of a row than the teams of a block take at once."""
+    attend(400 + D, [131072, 70000], [1, 1], 2 * heads, heads, D, 256, F16)
+
+
+@pytest.mark.parametrize("D", [64, 96])
+def test_splits_with_missing_pages_nan_and_nothing_to_see(D, rows):
+    """On contexts that are split: a split made of missing pages, a NaN in a later split, sequences of which nothing is seen."""
+    g, page, l, H = rng(70 + D), 64, 6000, 2
+    cache, table = filled(g, [l, l], H, page, D)
+    k, v = dense(cache, table, 0, l)
+    q = normal(g, 4, 4, D, dtype=BF16)
+    damaged = table.clone()
+    damaged[0, 16:40] = -3                                # tokens 1024 .. 2559
+    damaged[0, 70] = 1 << 30
+    keep = np.r_[0:1024, 2560:4480, 4544:l]
+    start = ints([0, 2, 4])
+    out = B.apnn_kv_attention(cache, q, ints([l, 0]), damaged, 0.1, q_start=start, max_q=2)
+    for i in range(2):
+        seen = keep[keep <= l - 2 + i]
+        for h in range(4):
+            want, spread, _ = O.attention(f64(q[i:i + 1, h]), k[seen, h // 2], v[seen, h // 2], len(seen) - 1, 0.1)
+            close(out[i, h], want[0], BF16, 2.0 ** -10 * spread[0] + 1e-6)
+    assert (out[2:] == 0).all()
+    bad = torch.randn(1, H, D, device="cuda")
+    bad[0, 1, 3] = float("inf")
+    t = l - 1                                             # seen by the second query only
+    B.apnn_kv_append(cache, bad, bad, (table[0, t // page].long() * page + t % page).reshape(1))
+    out = B.apnn_kv_attention(cache, q, ints([l, 1]), damaged, 0.1, q_start=start, max_q=2)
+    nan = torch.isnan(out).all(-1).cpu().numpy()
+    want = np.zeros((4, 4), bool)
+    want[1, 2:] = True
+    np.testing.assert_array_equal(nan, want)
+    np.testing.assert_array_equal(torch.isnan(out).any(-1).cpu().numpy(), want)
+    assert (out[2] == 0).all() and (out[3] != 0).any()
+    assert (B.apnn_kv_attention(cache, q, ints([l, l]), torch.full_like(table, -1), 0.1, q_start=start, max_q=2) == 0).all()
+
+
 # two, three and four tiles of channels a block with as many of tokens, sizes that end inside a tile
 WIDE = [(20, 6150, 200), (40, 9300, 333), (17, 12301, 129), (48, 6200, 64), (33, 6145, 1000), (45, 12300, 130), (64, 6161, 100), (60, 9217, 65), (50, 12305, 47),
         (31, 9999, 77), (100, 2601, 77), (128, 5200, 300), (128, 7700, 300), (66, 5121, 500), (127, 10240, 33)]
