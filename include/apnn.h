@@ -336,7 +336,8 @@ typedef struct {
     int64_t table_rows;
     const int32_t *position_dev;/* [tokens] */
     /* Queries rotated like the keys and written to q_out; q_heads 0: none.
-     * q_out may be q itself, with the same strides; otherwise they must not overlap. */
+     * q_out may be q itself, with the same strides; otherwise it must not overlap q.  It must
+     * not overlap k or v. */
     int q_heads;
     const void *q_dev;          /* [tokens][q_heads][D] */
     void *q_out_dev;
@@ -350,7 +351,7 @@ typedef struct {
  * A (token, head) whose rotated key or value is not finite in fp32 is held as NaN.
  * A token whose slot lies outside the cache (a negative one marks padding), or whose
  * position lies outside the table (looked at if rot > 0), is left out: nothing of it is
- * written, q_out neither.  Slots of one call must differ: of two tokens in one slot,
+ * written, and its queries in q_out are left as they were.  Slots of one call must differ: of two tokens in one slot,
  * that slot holds a mixture. */
 int apnn_kv_append(const apnn_kv_cache *cache, const apnn_kv_tokens *tokens, void *stream);
 

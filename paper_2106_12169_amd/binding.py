@@ -373,7 +373,7 @@ def apnn_token_pitch(K: int) -> int:
 
 def apnn_quantize_tokens(src: torch.Tensor, codes: Optional[torch.Tensor] = None,
                          scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """src: rows x K (float32, float16 or bfloat16; any row stride) -> int8 codes [rows][apnn_token_pitch(K)] and fp32 scales
+    """src: rows x K (float32, float16 or bfloat16; any row stride from K up) -> int8 codes [rows][apnn_token_pitch(K)] and fp32 scales
     [rows], row = codes * scale.  Activations of a call, and weights (output channels x K) once."""
     return _N.quantize_tokens(src, codes, scale)
 
@@ -381,7 +381,7 @@ def apnn_quantize_tokens(src: torch.Tensor, codes: Optional[torch.Tensor] = None
 def apnn_gemm_scaled(X: torch.Tensor, x_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, K: int, *,
                      bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """X: M x K, W: N x K codes as apnn_quantize_tokens lays them out -> M x N of `dtype` (or into `out`, of any row stride)."""
+    """X: M x K, W: N x K codes as apnn_quantize_tokens lays them out -> M x N of `dtype` (or into `out`, of any row stride from N up)."""
     return _N.gemm_scaled(X, x_scale, W, w_scale, K, bias, out, dtype)
 
 
@@ -416,7 +416,8 @@ def apnn_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torc
                    q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """k, v: tokens x heads x D into the cache's slots (int64, page * page_size + place; negative: padding, left out).
     table (fp32, positions x rot: cosines, then sines) and positions (int32) rotate the first rot channels of keys and of q
-    (tokens x query heads x D).  Returns the rotated queries (q_out, which may be q itself; made if not given), None without q."""
+    (tokens x query heads x D).  Returns the rotated queries (q_out, which may be q itself; made if not given), None without q.  Queries of
+    tokens that are left out are not written: as they were in a given q_out, whatever the memory held in one that is made."""
     return _N.kv_append(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, k, v, slots, positions, table, interleaved, q, q_out)
 
 
@@ -435,10 +436,11 @@ def apnn_kv_attention(cache: KVCache, q: torch.Tensor, lens: torch.Tensor, pages
                       q_start: Optional[torch.Tensor] = None, max_q: Optional[int] = None, out: Optional[torch.Tensor] = None,
                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q: tokens x query heads x D (float16 or bfloat16) -> the same, attended.  lens: int32, tokens in the cache of each
-    sequence, its queries' own among them; pages: int32, sequences x max_pages.  q_start: int32, sequences + 1, where each
-    sequence's queries begin (None: one query each); max_q: a bound on the queries of a sequence (default: all of them,
-    which is right but spreads the work for one sequence that has them all).  Rows of `out` that no sequence has are left as
-    they were.  workspace: uint8, for the caller to keep (default: allocated for the call)."""
+    sequence, its queries' own among them; pages: int32, sequences x max_pages (how the work is split goes by this width: best
+    no wider than contexts can get).  q_start: int32, sequences + 1, where each sequence's queries begin (None: one query each);
+    max_q: a bound on the queries of a sequence (default: all of them, which is right but spreads the work for one sequence
+    that has them all).  Rows of `out` that no sequence has, and queries beyond max_q, are left as they were; without `out`, they
+    hold whatever the memory held.  workspace: uint8, for the caller to keep (default: allocated for the call)."""
     return _N.kv_attention(cache.k_codes, cache.k_scale, cache.v_codes, cache.v_scale, q, lens, pages, scale, q_start, max_q, out, workspace)
 
 

@@ -210,6 +210,11 @@ constexpr float kSlack = 8.0f;
 // Weights are 2^(score - maximum + kLift): at most 2^15, which fp16 holds, and as far above fp16's smallest step as that allows.  A weight
 // keeps fp16's 11 bits down to 2^-21 of the largest one and is lost only below 2^-32 of it; without the lift, 2^-14 and 2^-25, tokens
 // 17 nats below a single large one lost 44 % and at 17.4 everything, however many they were.  Weights' sums have the same factor.
+//
+// One fp16 number a weight: its rounding weighs as much as an fp16 result's own (rms error 2.9e-4 of the result, 2.05e-4 with exact
+// weights) and an eighth of a bf16 result's.  What it leaves in a second fp16 number and a second product makes the error that of exact
+// weights, but 48 x 8192 tokens take 65.1 us instead of 62.9, 2 x 131072 27.6 instead of 26.7, 1 x 500 5.92 instead of 5.64 and prompts 300
+// instead of 223.
 constexpr float kLift = 7.0f;
 
 // Tokens of a split: a tile's tokens over `splits`, whole turns of the block's waves, and no fewer than pay for the joining.
@@ -228,7 +233,8 @@ template <int D> __device__ __forceinline__ float *part_of(const AttentionArgs &
 
 // 16 query rows of one cache head against one split of the sequence, the four waves taking 32 tokens each in turn.
 //
-// Bound by memory: (D / 2 + D / 32) 2 bytes a token and cache head; 4.7 to 5.2 TB/s from 100 MB of codes up.  A wave has the next 32 tokens' codes in flight, in
+// Bound by memory: (D / 2 + D / 32) 2 bytes a token and cache head.  Of codes not read just before, 103 MB take 25.8 us and 242 MB in contexts of
+// every length up to 8192 58 (4.0, 4.2 TB/s); 430 to 860 MB in contexts of one length 4.7 to 5.3 TB/s.  A wave has the next 32 tokens' codes in flight, in
 // registers, while it works on the current ones, and the page numbers of the 32 after those; four blocks of four waves fit
 // a compute unit, 70 KB in flight.  LDS is only the way V is transposed, private to a wave: no barrier before the end.
 template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256 ? 2 : 4) void kv_attention_kernel(AttentionArgs a, int64_t first)
@@ -443,7 +449,8 @@ template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<
 //
 // Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (two where
 // D = 256) overlap: 34 % and 39 % of the cycles with two blocks of two tiles each, 245 us for prompts of up to 2048 tokens on
-// contexts of up to 4096, 32 heads on 8 of D = 128; 215 to 219 us (860 TFLOP/s) as it is.  The tokens' codes are converted to LDS once for
+// contexts of up to 4096, 32 heads on 8 of D = 128; 216 to 223 us over boxes (840 to 870 TFLOP/s; 229 in a kernel trace) as it is.  D = 128 spills
+// one register, D = 256 21 to 26 (two prompts of 4096, 16 heads on 4: 358 us, 768 TFLOP/s).  The tokens' codes are converted to LDS once for
 // all rows, those of the next tile on their way meanwhile.  As for 16 rows, scores are computed transposed and the weights stay
 // in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
 // values are read in that order.
