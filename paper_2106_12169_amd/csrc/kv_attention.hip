@@ -171,16 +171,16 @@ __device__ __forceinline__ Rows find_rows(const AttentionArgs &a, int64_t b, int
     return x;
 }
 
-// What 1 / (sum of weights) is for a query whose weights sum to 0: 0 if no token that it sees is in a page of the cache, NaN if all scores are -inf or
-// the maximum is beyond fp32 (infinite queries, sums and scales out of range).  The loops over tokens need not know; this is looked up at the end.
-__device__ __forceinline__ float inverse_of_nothing(const AttentionArgs &a, const Rows &x, int64_t seq, int i)
+// The maximum of a row of which no weight is left, over the tokens from `begin` up to `end`: -inf if it sees none of them, and a number below every
+// other if one is in a page of the cache (its scores are then all -inf: infinite queries, sums out of range).  A row of which -inf is the maximum of
+// all its parts gets zeros, one whose weights sum to 0 all the same NaN.  The loops over tokens need not know; this is looked up behind them.
+__device__ __forceinline__ float top_of_nothing(const AttentionArgs &a, int64_t seq, int begin, int end)
 {
-    const int seen = seen_by(x, i);
-    for (int p = 0; p << a.page_shift < seen; ++p) {
+    for (int p = begin >> a.page_shift; p << a.page_shift < end; ++p) {
         const int page = a.d.page_dev[seq * a.d.max_pages + p];
-        if (page >= 0 && page < a.c.pages) return __uint_as_float(0x7FC00000u);
+        if (page >= 0 && page < a.c.pages) return -3.402823466e38f;
     }
-    return 0.0f;
+    return -INFINITY;
 }
 
 // Tile, cache head and sequence of a block.  Heads and sequences change fastest: blocks go to the eight XCDs in turn, so that the
@@ -399,6 +399,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    if (top == -INFINITY && live) top = top_of_nothing(a, b, begin + wave * tokens, min(end, seen + 4 * quarter));
 
     // the four waves' parts, joined on their common maximum
     if (quarter == 0) {
@@ -429,7 +430,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
                 part[D + 1] = l;
             }
         } else {
-            const float inv = l == 0.0f ? inverse_of_nothing(a, x, b, ri) : 1.0f / l;
+            const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
             T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + ch;
             for (int j = 0; j < 4; ++j) to[j] = static_cast<T>(o[j] * inv);
         }
@@ -449,8 +450,8 @@ template <int D> constexpr int kManyTile = 64 * (kManyKeyRow<D> + kManyValueRow<
 //
 // Bound by the matrix unit and the vector instructions of the softmax, which the three blocks of a compute unit (two where
 // D = 256) overlap: 34 % and 39 % of the cycles with two blocks of two tiles each, 245 us for prompts of up to 2048 tokens on
-// contexts of up to 4096, 32 heads on 8 of D = 128; 216 to 223 us over boxes (840 to 870 TFLOP/s; 229 in a kernel trace) as it is.  D = 128 spills
-// one register, D = 256 21 to 26 (two prompts of 4096, 16 heads on 4: 358 us, 768 TFLOP/s).  The tokens' codes are converted to LDS once for
+// contexts of up to 4096, 32 heads on 8 of D = 128; 214 to 223 us over boxes (840 to 875 TFLOP/s; 229 in a kernel trace) as it is.  D = 128 spills
+// up to four registers, D = 256 21 to 26 (two prompts of 4096, 16 heads on 4: 358 us, 768 TFLOP/s).  The tokens' codes are converted to LDS once for
 // all rows, those of the next tile on their way meanwhile.  As for 16 rows, scores are computed transposed and the weights stay
 // in their registers: the 32 x 32 instruction leaves a lane with tokens 8 (i / 4) + 4 half + i % 4 of its column, and the
 // values are read in that order.
@@ -624,6 +625,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
     const u32x2_t two = both_halves(sum);
     sum = __uint_as_float(two[0]) + __uint_as_float(two[1]);
     if (!live) return;
+    if (top == -INFINITY) top = top_of_nothing(a, place.seq, begin, min(end, seen));
     if (SPLIT) {
         float *part = part_of<D>(a, unit, split, 32 * wave + c);
 #pragma unroll
@@ -637,7 +639,7 @@ template <class T, int D, bool SPLIT> __global__ __launch_bounds__(256, D == 256
         }
         return;
     }
-    const float inv = sum == 0.0f ? inverse_of_nothing(a, x, place.seq, i) : 1.0f / sum;
+    const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;
     T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + i) * a.d.out_token_stride + (head * a.group + (r - i * a.group)) * a.d.out_head_stride + 4 * half;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -705,9 +707,8 @@ template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_a
         }
         __syncthreads();
         if (team) return;
-        float top = -INFINITY;
-        for (int s = 0; s < teams; ++s) top = fmaxf(top, tops[s]);
-        const float base = top == -INFINITY ? 0.0f : top;
+        for (int s = 0; s < teams; ++s) m = fmaxf(m, tops[s]);
+        const float base = m == -INFINITY ? 0.0f : m;
         o = f32x4_t{};
         l = 0.0f;
         for (int s = 0; s < teams; ++s) {
@@ -716,7 +717,7 @@ template <class T, int D, bool MANY> __global__ __launch_bounds__(256) void kv_a
             l += weights[s] * f;
         }
     }
-    const float inv = l == 0.0f ? inverse_of_nothing(a, x, place.seq, ri) : 1.0f / l;
+    const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
     T *to = static_cast<T *>(a.d.out_dev) + (x.q0 + ri) * a.d.out_token_stride + (head * a.group + (rr - ri * a.group)) * a.d.out_head_stride + 4 * lane;
     T y[4];
 #pragma unroll

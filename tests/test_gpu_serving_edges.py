@@ -101,6 +101,24 @@ def test_queries_and_scores_beyond_range_give_nan(l, dtype, rows):
     assert torch.equal(B.apnn_kv_attention(cache, q, ints([l]), table, -1e35), q)
 
 
+def test_parts_without_a_number_join_with_those_that_have_one(rows):
+    """Scores of -inf in one part of a context that is split and finite ones in another: the former have no weight; none at all gives NaN."""
+    l, D = 6000, 64
+    cache = B.KVCache.empty(l // 16, 1, 16, D)
+    k, v = torch.zeros((l, 1, D), device="cuda"), torch.zeros((l, 1, D), device="cuda")
+    k[:3000], k[3000:], v[:3000], v[3000:] = -6 * 2.0 ** 13, 1.0, 3.0, 2.0
+    B.apnn_kv_append(cache, k, v, torch.arange(l, device="cuda"))
+    table = torch.arange(l // 16, dtype=torch.int32, device="cuda").reshape(1, -1)
+    q = torch.full((2, 2, D), 2.0 ** 115, dtype=BF16, device="cuda")   # -6 2^13 2^115 D: out of range; 2^115 D is not
+    start = ints([0, 2])
+    assert (B.apnn_kv_attention(cache, q, ints([l]), table, 2.0 ** -115, q_start=start, max_q=2) == 2).all()
+    assert torch.isnan(B.apnn_kv_attention(cache, q, ints([3000]), table, 2.0 ** -115, q_start=start, max_q=2)).all()
+    some = table.clone()
+    some[0, :3000 // 16 + 1] = -1                         # tokens 0 .. 3007 are nowhere
+    assert (B.apnn_kv_attention(cache, q, ints([3000]), some, 2.0 ** -115, q_start=start, max_q=2) == 0).all()
+    assert (B.apnn_kv_attention(cache, q, ints([l]), some, 2.0 ** -115, q_start=start, max_q=2) == 2).all()
+
+
 @pytest.mark.parametrize("l, news", [(300, 40), (300, 200), (3000, 4)])
 def test_values_of_unseen_tokens_may_be_any_bytes(l, news, rows):
     """Value scale bytes that append never writes, in tokens that stand after the query: nothing of them reaches it."""
