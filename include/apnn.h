@@ -373,7 +373,7 @@ typedef struct {
     const int32_t *page_dev;    /* [seqs][max_pages]: token t of sequence b is in page page[b][t / page_size] */
     int64_t max_pages;
     int64_t max_q;              /* no sequence has more queries (1 if q_start_dev is NULL) */
-    float scale;                /* of the scores, finite */
+    float scale;                /* of the scores, at most 2^127 in magnitude */
 } apnn_kv_attention_desc;
 
 /* out = sum_t softmax_t(scale * q . k_t) v_t for every query head.  Query i of the n of a

@@ -746,7 +746,7 @@ int check_attention(const char *who, const apnn_kv_attention_desc *d, const apnn
     if (d->q_heads < 1 || d->q_heads % c->heads) return fail(APNN_ERR_INVALID_ARG, "%s: %d query heads over %d cache heads", who, d->q_heads, c->heads);
     const double rows = static_cast<double>(d->q_start_dev ? (d->max_q < d->tokens ? d->max_q : d->tokens) : 1) * d->q_heads;
     if ((rows / 16 + c->heads) * d->seqs > 1e12) return fail(APNN_ERR_UNSUPPORTED, "%s: %lld sequences of up to %lld queries", who, (long long)d->seqs, (long long)d->max_q);
-    if (!(d->scale - d->scale == 0.0f)) return fail(APNN_ERR_INVALID_ARG, "%s: scale is not finite", who);
+    if (!(fabsf(d->scale) <= 0x1p127f)) return fail(APNN_ERR_INVALID_ARG, "%s: scale = %g, at most 2^127 in magnitude", who, static_cast<double>(d->scale));
     if (!d->q_start_dev && d->tokens < d->seqs) return fail(APNN_ERR_INVALID_ARG, "%s: one query each for %lld sequences, %lld rows", who, (long long)d->seqs, (long long)d->tokens);
     return APNN_OK;
 }

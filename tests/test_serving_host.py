@@ -167,3 +167,11 @@ def test_sizes_beyond_32_bits_are_refused_and_not_cut_off(at):
         bad[at] += far
         with pytest.raises(B.ApnnError):
             B.native().kv_attention_workspace(*bad)
+
+
+@pytest.mark.parametrize("scale, status", [(1.5 * 2.0 ** 127, ARG), (-3e38, ARG), (2.0 ** 127, 0), (-(2.0 ** 127), 0), (1e-45, 0)])
+def test_scales_that_leave_no_room_for_powers_of_two_are_refused(scale, status):
+    """Scores are taken in powers of two: the scale times log2(e) has to be a number too."""
+    d = attention(scale=scale, tokens=0, seqs=0)
+    assert B.lib().apnn_kv_attention(C.byref(d), C.byref(cache()), None, 0, None) == status
+    assert ("scale" in last()) == bool(status)
